@@ -264,6 +264,121 @@ ps_status ps_init_head(ps_ctx* ctx, const ps_head_weights* w);
 ps_status ps_step_tokens(ps_ctx* ctx, const ps_seq* seqs, int32_t n_seqs, const int32_t* token_ids, int32_t* next_tokens,
                          float* logits, float* hidden, ps_step_stats* stats, float* ms_parts);
 
+/* ---- drafted tokens (Sec. 2.1: a decode step makes one token; a draft lets it check several) --------------------
+ *
+ * A request's new tokens may form a tree: each token ("node") hangs below an earlier node or below the cached prefix, and
+ * attends to the prefix, to its ancestors and to itself.  Node i of a sequence is stored in the cache at position prefix + i
+ * (prefix = kv_len - n_new) and rotated for position prefix + its depth (0 for a node below the prefix).  After the step the
+ * caller keeps one branch (ps_tree_keep) and goes on behind it.  A plain chain is an ordinary prefill chunk or, of one token, a
+ * decode; a batch may mix all of them.
+ *
+ * A ps_tree holds what a batch of trees needs on the device (positions, slots, page lists, attention work list, masks, partial
+ * sums): planned once, it serves all layers.  Except ps_tree_plan and the first ps_verify_tokens of a size, the calls below only launch
+ * kernels, on the context's stream, and may be captured into a HIP graph; such a graph is valid until its tree is planned again or
+ * destroyed, and is to be replayed in order with the context's other work, whose buffers it shares.  The calls may be made while another
+ * device is current. */
+typedef struct ps_tree ps_tree;
+
+#define PS_TREE_PAD (-2)        /* parent of a padding node */
+#define PS_TREE_MAX_NODES 1024  /* of a sequence whose new tokens are not a plain chain */
+
+/* Element types of tensors that come in more than one. */
+#define PS_F32 0
+#define PS_BF16 1
+
+/* An empty tree.  Errors: PS_EINVAL, PS_ENOMEM. */
+ps_status ps_tree_create(ps_ctx* ctx, ps_tree** out);
+
+/* Free it (waits for the device); null is a no-op.  Its context may be gone already. */
+void ps_tree_destroy(ps_tree* tree);
+
+/* Plan the batch: seqs as for ps_step (n_seqs == 0: an empty batch), parents (host, [T], concatenated like the tokens; null: every
+ * sequence a chain): parents[i] of a sequence is the index, within the sequence's new tokens, of an earlier node, or -1 below the prefix,
+ * or PS_TREE_PAD for padding: such a node has a slot (rotated for position prefix) but sees nothing and is seen by nothing, and its
+ * attention output is zero.  Replaces what the tree held; work enqueued before still runs on that.  The arrays may be freed when the
+ * call returns.  Device and pinned memory grows as needed (a larger batch than any before waits for the stream).  On a host-only context
+ * only the host side is planned.  On an error the tree is empty.
+ * Errors: PS_EINVAL / PS_ERANGE for a malformed batch or parent (not an earlier node, or padding), PS_ENOMEM. */
+ps_status ps_tree_plan(ps_ctx* ctx, ps_tree* tree, const ps_seq* seqs, int32_t n_seqs, const int32_t* parents);
+
+/* Integer side of the plan, host arrays as in ps_step_indices (positions: prefix + depth).  Errors: PS_EINVAL. */
+ps_status ps_tree_indices(ps_ctx* ctx, const ps_tree* tree, int32_t* cu_seqlens, int32_t* positions, int32_t* slot_mapping);
+
+/* Gains of a layer whose queries and keys are normalised head by head before the rotation: device bf16 [head_dim] each, copied (the
+ * caller may free them once ps_sync() has returned).  Both null: the layer does not normalise (the default).  All steps obey it.
+ * Errors: PS_ERANGE (layer), PS_EINVAL (one null), PS_ENOMEM, PS_ESTATE (host-only context). */
+ps_status ps_init_qk_norm(ps_ctx* ctx, int32_t layer, const void* g_q, const void* g_k);
+
+/* A layer's projections -> rotated queries, and keys and values in the cache: for each query and key head u' = u * gain / sqrt(mean(u^2) +
+ * rms_eps) (layers with ps_init_qk_norm), rotated for the token's position; everything in fp32 and rounded to bf16 once.  qkv: device, T
+ * rows of (n_q + 2 n_kv) * head_dim values of `dtype` (PS_F32 or PS_BF16), queries, keys, values, ld elements from one row to the next;
+ * q: device bf16 [T][n_q][head_dim].  Both 16-byte aligned, rows of qkv too.
+ * Errors: PS_EINVAL, PS_ERANGE (layer), PS_ESTATE (no plan, or one for another context or pool; no pool). */
+ps_status ps_qk_norm_rope(ps_ctx* ctx, int32_t layer, const ps_tree* tree, const void* qkv, int32_t dtype, int64_t ld, void* q);
+
+/* out[i] = sum over what node i sees of softmax(q_i . k / sqrt(head_dim)) v, query head h reading KV head h / (n_q / n_kv); the nodes' own
+ * keys and values are in the cache (ps_qk_norm_rope).  q, out: device bf16, T rows of n_q * head_dim values, ldq and ldo elements from
+ * one row to the next, 16-byte aligned, rows too; they do not overlap.  Cache entries that a node does not see do not reach its row,
+ * whatever they hold; a node's row depends on no other node's query.  Weights are rounded to bf16 for the matrix units, sums are fp32.
+ * Errors as ps_qk_norm_rope. */
+ps_status ps_tree_attention(ps_ctx* ctx, int32_t layer, const ps_tree* tree, const void* q, int64_t ldq, void* out, int64_t ldo);
+
+/* Keep of every sequence the nodes nodes[..] (host; n_keep[s] of sequence s, concatenated, ascending): their keys and values move to the
+ * positions prefix, prefix + 1, ... in all KV slots.  The branch's next position is then prefix + n_keep[s]; what lies behind is stale.
+ * A node whose place it already is does not move.  The call is to be made once for a plan.
+ * Errors: PS_EINVAL (null, not ascending), PS_ERANGE (no such node), PS_ESTATE as ps_qk_norm_rope; nothing has been launched. */
+ps_status ps_tree_keep(ps_ctx* ctx, const ps_tree* tree, const int32_t* n_keep, const int32_t* nodes);
+
+/* Rules on the logits of n_rows rows.  All pointers are device memory, any group may be null.  A request ("list") has a history of token
+ * ids and numbers that go with it; a row belongs to a list.  With z the row's logit of a token:
+ *   1. token in the list's history, or in the row's branch:   z = z > 0 ? z / repetition : z * repetition
+ *   2. z = z - frequency * n, n = times in the history from output_begin on and in the branch
+ *   3. n > 0:  z = z - presence
+ *   4. z = z + bias (of a token that is listed twice, the later entry)
+ *   5. the mask does not allow the token:  z = -inf, whatever it was
+ * in fp32, each operation rounded.  Ids outside [0, vocab) are passed over, offsets are clamped to the arrays' lengths. */
+typedef struct {
+    int32_t n_lists;                 /* 0: only the mask applies */
+    int32_t n_history;               /* entries of history */
+    const int32_t* history;          /* list l: entries [history_begin[l], history_begin[l + 1]), the prompt first */
+    const int32_t* history_begin;    /* [n_lists + 1] */
+    const int32_t* output_begin;     /* [n_lists] entry where the list's output begins (null: all of it is output) */
+    const float *repetition, *frequency, *presence;  /* [n_lists] (null: 1, 0, 0); repetition > 0 */
+    const int32_t* bias_token;       /* list l: entries [bias_begin[l], bias_begin[l + 1]) */
+    const float* bias_value;
+    const int32_t* bias_begin;       /* [n_lists + 1] */
+    int32_t n_biases;                /* entries of bias_token */
+    int32_t n_masks;
+    const uint32_t* mask;            /* n_masks rows, token t allowed: bit t % 32 of word t / 32 */
+    int64_t mask_stride;             /* words from one row to the next, >= ceil(vocab / 32) */
+    const int32_t* mask_row;         /* [n_rows] mask of the row, negative: none, >= n_masks: nothing is allowed; null: row i has mask i */
+    const int32_t* row_list;         /* [n_rows] list of the row (outside [0, n_lists): none); null: row i has list i, n_lists == n_rows */
+    const int32_t* row_token;        /* [n_rows] or null: a row is a node; its branch is its own token and those of the rows above it */
+    const int32_t* row_prev;         /* [n_rows] or null: the row above a row, an earlier one, or negative */
+} ps_logit_rules;
+
+/* Apply the rules to logits (device, n_rows rows of vocab <= 2^20 values of `dtype`, ld elements from one row to the next) and pick: next [n_rows]
+ * the index of the largest, the lowest index among equal ones (a NaN is never it), or -1 where nothing is above -inf; logprob
+ * [n_rows] fp32 its log-probability among the changed logits (-inf with next = -1; NaN if one of them is NaN or +inf); out fp32 the
+ * changed logits, ldo elements from one row to the next (may be logits itself if that is fp32 and ld == ldo).  Outputs are device
+ * memory, any may be null; rules null: none.  Needs no pool and no weights.  Errors: PS_EINVAL, PS_ERANGE, PS_ESTATE (host-only context). */
+ps_status ps_pick_tokens(ps_ctx* ctx, const void* logits, int32_t dtype, int64_t ld, int32_t n_rows, int32_t vocab, const ps_logit_rules* rules,
+                         float* out, int64_t ldo, int32_t* next_tokens, float* logprobs);
+
+/* One full-model step over a batch of trees: as ps_step_tokens with ps_qk_norm_rope and ps_tree_attention in its layers and ps_pick_tokens
+ * over all T nodes.  token_ids: HOST [T].  rules (null: none): n_lists 0 or the batch's number of sequences, list s belonging to sequence s; row_list,
+ * row_token and row_prev null (the nodes' branches count as output); mask_row and masks as for T rows.  Outputs, device, any may be null:
+ * next_tokens int32 [T], logprobs fp32 [T], logits fp32 [T][vocab] (changed by the rules), hidden fp32 [T][hidden].  Rows of padding
+ * hold numbers without meaning.  Errors: as ps_step_tokens and ps_pick_tokens; PS_ESTATE as ps_qk_norm_rope. */
+ps_status ps_verify_tokens(ps_ctx* ctx, const ps_tree* tree, const int32_t* token_ids, const ps_logit_rules* rules, int32_t* next_tokens,
+                           float* logprobs, float* logits, float* hidden);
+
+/* Device address and size of the KV pool ([KV slot][page][kv head][K, V][16 * head_dim] bf16), for callers that snapshot pages or move
+ * them between devices as they are.  Element (token i of its page, value e) of a head's 16 * head_dim keys lies at
+ * ((e / 8) * 16 + i) * 8 + e % 8, of its values at (((e / 32) * 4 + i / 4) * 16 + e % 16) * 8 + (e / 16 % 2) * 4 + i % 4.
+ * Valid until the next ps_kv_alloc.  Errors: PS_EINVAL, PS_ESTATE (no pool, host-only context). */
+ps_status ps_kv_pool(ps_ctx* ctx, void** pool, int64_t* bytes);
+
 /* Integer side of a step, host only, no launch: cu_seqlens [n_seqs+1] (exclusive scan of
  * n_new), positions [T] (kv_len - n_new + i), slot_mapping [T] (page id * 16 + position
  * % 16): the cache slots the step's KV append writes.  Output arrays are host memory; any

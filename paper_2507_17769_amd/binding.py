@@ -26,6 +26,9 @@ PS_N_STAGES = 8
 PS_GRID_MAX_DRAWS = 8
 PS_STATIC_SCRATCH_BYTES = 64 << 20
 PS_FLAG_HOST_ONLY = 1
+PS_TREE_PAD = -2
+PS_TREE_MAX_NODES = 1024
+PS_F32, PS_BF16 = 0, 1
 STAGE_NAMES = ["rmsnorm_attn", "gemm_qkv", "rope_append", "attention", "gemm_o", "rmsnorm_ffn", "gemm_gate_up", "gemm_down"]
 
 
@@ -82,6 +85,14 @@ class ps_taps(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("xn", "q", "attn", "x1", "xn2", "act", "x_in", "x_out")]
 
 
+class ps_logit_rules(C.Structure):
+    _fields_ = [("n_lists", C.c_int32), ("n_history", C.c_int32), ("history", C.c_void_p), ("history_begin", C.c_void_p),
+                ("output_begin", C.c_void_p), ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("bias_token", C.c_void_p), ("bias_value", C.c_void_p), ("bias_begin", C.c_void_p), ("n_biases", C.c_int32),
+                ("n_masks", C.c_int32), ("mask", C.c_void_p), ("mask_stride", C.c_int64), ("mask_row", C.c_void_p),
+                ("row_list", C.c_void_p), ("row_token", C.c_void_p), ("row_prev", C.c_void_p)]
+
+
 class ps_grid_cell_spec(C.Structure):
     _fields_ = [("chunk", C.c_int32), ("n_decode", C.c_int32), ("n_draws", C.c_int32),
                 ("chunk_prefix", C.POINTER(C.c_int32)), ("decode_kv", C.POINTER(C.c_int32))]
@@ -116,6 +127,17 @@ _SIGS = {
     "ps_step_static": (C.c_int, [_P, C.POINTER(ps_seq), C.c_int32, _P, _P]),
     "ps_init_head": (C.c_int, [_P, C.POINTER(ps_head_weights)]),
     "ps_step_tokens": (C.c_int, [_P, C.POINTER(ps_seq), C.c_int32, _I32P, _P, _P, _P, C.POINTER(ps_step_stats), C.POINTER(C.c_float)]),
+    "ps_tree_create": (C.c_int, [_P, C.POINTER(_P)]),
+    "ps_tree_destroy": (None, [_P]),
+    "ps_tree_plan": (C.c_int, [_P, _P, C.POINTER(ps_seq), C.c_int32, _I32P]),
+    "ps_tree_indices": (C.c_int, [_P, _P, _I32P, _I32P, _I32P]),
+    "ps_init_qk_norm": (C.c_int, [_P, C.c_int32, _P, _P]),
+    "ps_qk_norm_rope": (C.c_int, [_P, C.c_int32, _P, _P, C.c_int32, C.c_int64, _P]),
+    "ps_tree_attention": (C.c_int, [_P, C.c_int32, _P, _P, C.c_int64, _P, C.c_int64]),
+    "ps_tree_keep": (C.c_int, [_P, _P, _I32P, _I32P]),
+    "ps_pick_tokens": (C.c_int, [_P, _P, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.POINTER(ps_logit_rules), _P, C.c_int64, _P, _P]),
+    "ps_verify_tokens": (C.c_int, [_P, _P, _I32P, C.POINTER(ps_logit_rules), _P, _P, _P, _P]),
+    "ps_kv_pool": (C.c_int, [_P, C.POINTER(_P), C.POINTER(C.c_int64)]),
     "ps_step_indices": (C.c_int, [_P, C.POINTER(ps_seq), C.c_int32, _I32P, _I32P, _I32P]),
     "ps_plan_attention": (C.c_int, [_P, C.POINTER(ps_seq), C.c_int32, _I32P, C.c_int32, _I32P]),
     "ps_set_taps": (C.c_int, [_P, C.c_int32, C.POINTER(ps_taps)]),
@@ -308,6 +330,44 @@ class Context:
                                         pos.ctypes.data_as(_I32P), slots.ctypes.data_as(_I32P)))
         return cu, pos[:sa.n_tokens], slots[:sa.n_tokens]
 
+    def init_qk_norm(self, layer, g_q_ptr, g_k_ptr):
+        """Device bf16 [head_dim] gains; None, None: the layer's heads are not normalised."""
+        self._check(lib.ps_init_qk_norm(self.handle, layer, _P(g_q_ptr), _P(g_k_ptr)))
+
+    def qk_norm_rope(self, layer, tree, qkv_ptr, dtype, ld, q_ptr):
+        self._check(lib.ps_qk_norm_rope(self.handle, layer, tree.handle, _P(qkv_ptr), dtype, ld, _P(q_ptr)))
+
+    def tree_attention(self, layer, tree, q_ptr, ldq, out_ptr, ldo):
+        self._check(lib.ps_tree_attention(self.handle, layer, tree.handle, _P(q_ptr), ldq, _P(out_ptr), ldo))
+
+    def tree_keep(self, tree, kept):
+        """kept: for each sequence the nodes to keep, ascending."""
+        if len(kept) != tree.n_seqs:
+            raise ValueError("kept must hold one list of nodes per sequence")
+        lists = [_as_i32(k) for k in kept]
+        n = np.array([len(k) for k in lists], dtype=np.int32)
+        nodes = np.concatenate(lists) if lists else np.zeros(0, dtype=np.int32)
+        self._check(lib.ps_tree_keep(self.handle, tree.handle, n.ctypes.data_as(_I32P), nodes.ctypes.data_as(_I32P)))
+
+    def pick_tokens(self, logits_ptr, dtype, ld, n_rows, vocab, rules=None, out_ptr=None, ldo=0, next_ptr=None, logprob_ptr=None):
+        """rules: ps_logit_rules or None."""
+        self._check(lib.ps_pick_tokens(self.handle, _P(logits_ptr), dtype, ld, n_rows, vocab, C.byref(rules) if rules else None,
+                                       _P(out_ptr), ldo, _P(next_ptr), _P(logprob_ptr)))
+
+    def verify_tokens(self, tree, token_ids, rules=None, next_ptr=None, logprob_ptr=None, logits_ptr=None, hidden_ptr=None):
+        """token_ids: host int32 array [T]; rules: ps_logit_rules or None."""
+        ids = np.ascontiguousarray(token_ids, dtype=np.int32)
+        if ids.shape != (tree.n_tokens,):
+            raise ValueError("token_ids must hold one id per node")
+        self._check(lib.ps_verify_tokens(self.handle, tree.handle, ids.ctypes.data_as(_I32P), C.byref(rules) if rules else None,
+                                         _P(next_ptr), _P(logprob_ptr), _P(logits_ptr), _P(hidden_ptr)))
+
+    def kv_pool(self):
+        """(device address, bytes) of the KV pool."""
+        p, n = _P(), C.c_int64(0)
+        self._check(lib.ps_kv_pool(self.handle, C.byref(p), C.byref(n)))
+        return p.value, n.value
+
     def plan_attention(self, seqs):
         sa = seqs if isinstance(seqs, SeqArray) else SeqArray(seqs)
         n = C.c_int32(0)
@@ -360,6 +420,42 @@ class Context:
         opts = ps_grid_opts(warmup, iters)
         self._check(lib.ps_profile_grid(self.handle, specs, n, C.byref(opts), _P(x_in_ptr), _P(x_out_ptr), out))
         return [out[i] for i in range(n)]
+
+
+class Tree:
+    """Owns one ps_tree: a batch of token trees of a context."""
+
+    def __init__(self, ctx):
+        self.ctx = ctx
+        h = _P()
+        ctx._check(lib.ps_tree_create(ctx.handle, C.byref(h)))
+        self.handle = h
+        self.n_seqs = self.n_tokens = 0
+
+    def plan(self, seqs, parents=None):
+        """seqs as for Context.step; parents: host int32 array [T], concatenated (None: chains)."""
+        sa = seqs if isinstance(seqs, SeqArray) else SeqArray(seqs)
+        par = None if parents is None else np.ascontiguousarray(parents, dtype=np.int32)
+        if par is not None and par.shape != (sa.n_tokens,):
+            raise ValueError("parents must hold one entry per new token")
+        self.n_seqs = self.n_tokens = 0
+        self.ctx._check(lib.ps_tree_plan(self.ctx.handle, self.handle, sa.array, sa.n, None if par is None else par.ctypes.data_as(_I32P)))
+        self.n_seqs, self.n_tokens = sa.n, sa.n_tokens
+        return self
+
+    def indices(self):
+        cu = np.zeros(self.n_seqs + 1, dtype=np.int32)
+        pos, slots = np.zeros(max(self.n_tokens, 1), dtype=np.int32), np.zeros(max(self.n_tokens, 1), dtype=np.int32)
+        self.ctx._check(lib.ps_tree_indices(self.ctx.handle, self.handle, cu.ctypes.data_as(_I32P), pos.ctypes.data_as(_I32P), slots.ctypes.data_as(_I32P)))
+        return cu, pos[:self.n_tokens], slots[:self.n_tokens]
+
+    def destroy(self):
+        if getattr(self, "handle", None):
+            lib.ps_tree_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        self.destroy()
 
 
 # ---- polysched: host-side consumers of the latency profile (include/polysched.h) -------------

@@ -1,147 +1,17 @@
 // C-ABI of libpolystep: context, weights, paged KV pool + allocator, the mixed-batch step and
 // the latency-profile grid.  See include/polystep.h for the contract of every entry point.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
-#include <deque>
 #include <mutex>
 #include <new>
 
-#include "planner.h"
-#include "ps_common.h"
+#include "context.h"
 
 namespace ps {
-
 int attn_prefill_tokens_per_item(int G);
-
-struct LayerWeights {
-    bf16_t *wqkv_t = nullptr, *wo_t = nullptr, *wgu_t = nullptr, *wd_t = nullptr, *g_attn = nullptr, *g_ffn = nullptr;
-    bool ready = false;
-};
-
-struct Staging {  // pinned host buffer for one step's metadata
-    void* host = nullptr;
-    size_t bytes = 0;
-};
-
-// Memory of a step's four projections: the largest over them (see gemm_sizes).
-struct LayerNeeds {
-    size_t act_bytes, part_bytes, skfrag_bytes;
-    int skcnt_n;
-};
-
-// Where the buffers of a step lie in the static scratch array; `total` may exceed the array.
-struct StaticLayout {
-    size_t xn, q, attn, act, x1, xmid, part, part_o, part_ml, meta, skfrag, skcnt, total;
-    size_t act_bytes, part_bytes, skfrag_bytes;
-    int skcnt_n;
-};
-
-struct StepMemory {
-    GemmOptions gemm;      // of the layers' projections
-    LayerNeeds needs;
-    StaticLayout layout;
-};
-
-}  // namespace ps
-
-using namespace ps;
-
-struct ps_ctx {
-    ps_model_desc desc{};
-    bool host_only = false;
-    hipStream_t stream = nullptr;
-    std::string err;
-
-    std::vector<LayerWeights> layers;
-    float* rope_cs = nullptr;  // [max_position][d/2] (cos, sin)
-
-    // KV pool + allocator
-    bf16_t* pool = nullptr;
-    int n_pool_pages = -1;
-    int n_kv_slots = 0;
-    size_t slot_elems = 0;  // elements per physical layer slot
-    std::deque<int32_t> free_list;
-    std::unordered_map<int64_t, std::vector<int32_t>> owned;
-    std::vector<uint8_t> page_seen;
-
-    // workspaces
-    int cap_tokens = 0;
-    bf16_t *ws_xn = nullptr, *ws_q = nullptr, *ws_attn = nullptr, *ws_act = nullptr;
-    float *ws_x1 = nullptr, *ws_xmid = nullptr;
-    // model head (ps_init_head): embedding table, final gain, repacked output matrix; its workspaces
-    bf16_t *embedding = nullptr, *g_final = nullptr, *wout_t = nullptr;
-    int vocab = 0;
-    bool head_ready = false;
-    bf16_t* ws_embed = nullptr;   // [cap_tokens][hidden] bf16: embedding rows of the step's tokens
-    float* ws_final = nullptr;    // [cap_tokens][hidden] fp32: output of the last layer
-    float* ws_logits = nullptr;   // fp32 partials of the output projection, [splits][n_seqs][vocab]
-    size_t logits_bytes = 0;
-    int32_t* ws_next = nullptr;   // [cap] greedy tokens when the caller passes none
-    int next_cap = 0;
-    hipEvent_t ev_head[4] = {nullptr, nullptr, nullptr, nullptr};
-    float* ws_part = nullptr;  // fp32 GEMM partials [splits][T][N], shared by the three projections
-    size_t part_bytes = 0;
-    size_t act_bytes = 0;
-    float *part_o = nullptr, *part_ml = nullptr;
-    int cap_part_slots = 0;
-    // tiled GEMM: parked accumulators of partial K runs and one counter per tile (zero between launches)
-    float* ws_skfrag = nullptr;
-    size_t skfrag_bytes = 0;
-    int* ws_skcnt = nullptr;
-    int skcnt_n = 0;
-    // Device copies of the staging ring (same 8 slots).  The copy of step n+1's metadata runs on
-    // copy_stream while step n's kernels execute; the main stream only waits for the slot's event.
-    char* dev_meta = nullptr;
-    size_t dev_meta_slot = 0;  // bytes per slot
-    hipStream_t copy_stream = nullptr;
-    hipEvent_t meta_ready[8] = {};
-    // Ring of 8 pinned buffers in two halves.  One event per half, recorded after the half's last
-    // copy has been enqueued, tells when all four buffers of that half may be overwritten: one
-    // event record per four steps instead of one per step.
-    Staging staging[8];
-    hipEvent_t half_done[2] = {nullptr, nullptr};
-    bool half_pending[2] = {false, false};
-    int staging_next = 0;
-
-    // options / debug
-    int opt_attn_workers = 0;
-    int opt_attn_teams = 0;
-    int opt_attn_prefill_weight = 22;
-    int worker_slots = 2048;   // eight to a compute unit; without a device those of a whole MI355X
-    int opt_gemm_split_k = 0;
-    int opt_gemm_tile = 0;
-    int opt_gemm_whole_tiles = 0;
-    int opt_gemm_wreg = 0;
-    bool opt_poison = false;
-    int opt_only_layer = -1;
-    bool opt_out_f32 = false;
-    int tap_layer = -1;
-    ps_taps taps{};
-
-    // optional event pairs around every attention launch (see ps_attention_times)
-    int opt_time_attention = 0;   // 0 = off, N = bracket the attention launch of every Nth step
-    int64_t step_counter = 0;
-    std::vector<hipEvent_t> attn_ev;  // ring of 2 * ATTN_EV_PAIRS events
-    int attn_ev_count = 0;            // pairs recorded since the last ps_attention_times
-
-    // ps_step_static: this device's copy of the scratch array, a pinned ring for the metadata (allocated by ps_create)
-    unsigned char* static_scratch = nullptr;
-    char* static_host = nullptr;
-    hipEvent_t static_ev[4] = {nullptr, nullptr, nullptr, nullptr};
-    bool static_pending[4] = {false, false, false, false};
-    int static_next = 0;
-
-    // optional event pairs around the four projection launches of a layer (see ps_gemm_times)
-    int opt_time_gemm = 0;            // 0 = off, N = bracket them in every Nth step
-    std::vector<hipEvent_t> gemm_ev;  // ring of 8 * GEMM_EV_RECS events: record r holds pairs (qkv, o, gate/up, down)
-    int gemm_ev_count = 0;            // records (one per layer of a timed step) since the last ps_gemm_times
-
-    hipEvent_t ev[PS_N_STAGES * 2 + 2] = {};
-    bool have_events = false;
-    StepPlan plan;
-    StepMemory memory{};   // goes with it
-};
+}
 
 static constexpr int ATTN_EV_PAIRS = 2048;
 static constexpr int GEMM_EV_RECS = 1024;
@@ -158,40 +28,15 @@ static constexpr size_t STATIC_META_SLOT = 512u << 10;  // bytes of step metadat
 static constexpr int STATIC_META_SLOTS = 4;             // pinned host ring
 static thread_local std::string g_create_err;
 
-static ps_status fail(ps_ctx* c, ps_status s, const std::string& msg) {
+ps_status ps::fail(ps_ctx* c, ps_status s, const std::string& msg) {
     if (c) c->err = msg; else g_create_err = msg;
     return s;
 }
-static ps_status hip_fail(ps_ctx* c, hipError_t e, const char* what) {
+ps_status ps::hip_fail(ps_ctx* c, hipError_t e, const char* what) {
     return fail(c, e == hipErrorOutOfMemory ? PS_ENOMEM : PS_EDEVICE, std::string(what) + ": " + hipGetErrorString(e));
 }
-#define HIP_TRY(c, call)                                   \
-    do {                                                   \
-        hipError_t e__ = (call);                           \
-        if (e__ != hipSuccess) return hip_fail(c, e__, #call); \
-    } while (0)
 
-template <typename T>
-static ps_status dev_alloc(ps_ctx* c, T** p, size_t bytes, const char* what) {
-    *p = nullptr;
-    if (bytes == 0) return PS_OK;
-    hipError_t e = hipMalloc(reinterpret_cast<void**>(p), bytes);
-    if (e != hipSuccess) {
-        (void)hipGetLastError();
-        *p = nullptr;
-        return fail(c, PS_ENOMEM, std::string("device allocation failed for ") + what + " (" + std::to_string(bytes) + " bytes): " + hipGetErrorString(e));
-    }
-    return PS_OK;
-}
-template <typename T>
-static void dev_free(T*& p) {
-    if (p) (void)hipFree(p);
-    p = nullptr;
-}
-
-static int qkv_cols(const ps_model_desc& d) { return (d.n_q_heads + 2 * d.n_kv_heads) * d.head_dim; }
-
-static PlanConfig plan_config(const ps_ctx* c) {
+PlanConfig ps::plan_config(const ps_ctx* c) {
     PlanConfig pc;
     pc.n_kv_heads = c->desc.n_kv_heads;
     pc.group = c->desc.n_q_heads / c->desc.n_kv_heads;
@@ -227,6 +72,8 @@ extern "C" ps_status ps_create(const ps_model_desc* desc, void* hip_stream, ps_c
     ps_ctx* c = new (std::nothrow) ps_ctx();
     if (!c) return fail(nullptr, PS_ENOMEM, "ps_create: out of host memory");
     c->desc = d;
+    static std::atomic<uint64_t> next_id{1};
+    c->id = next_id++;
     if (!(c->desc.rms_eps > 0.f)) c->desc.rms_eps = 1e-5f;
     c->host_only = (d.flags & PS_FLAG_HOST_ONLY) != 0;
     c->stream = static_cast<hipStream_t>(hip_stream);
@@ -255,6 +102,7 @@ extern "C" ps_status ps_create(const ps_model_desc* desc, void* hip_stream, ps_c
         int dev = 0;
         e = hipGetDevice(&dev);
         if (e != hipSuccess) { ps_destroy(c); return hip_fail(nullptr, e, "hipGetDevice"); }
+        c->device = dev;
         if (dev < 0 || dev >= MAX_DEVICES) { ps_destroy(c); return fail(nullptr, PS_ERANGE, "ps_create: device index above 63"); }
         {
             std::lock_guard<std::mutex> lock(g_scratch_mutex);
@@ -286,7 +134,7 @@ extern "C" ps_status ps_sync(ps_ctx* c) {
     return PS_OK;
 }
 
-static void free_workspaces(ps_ctx* c) {
+void ps::free_workspaces(ps_ctx* c) {
     dev_free(c->ws_xn); dev_free(c->ws_q); dev_free(c->ws_attn); dev_free(c->ws_act);
     dev_free(c->ws_xmid); dev_free(c->ws_x1); dev_free(c->ws_part);
     dev_free(c->ws_embed); dev_free(c->ws_final);
@@ -300,6 +148,7 @@ extern "C" void ps_destroy(ps_ctx* c) {
         (void)hipStreamSynchronize(c->stream);
         for (auto& l : c->layers) {
             dev_free(l.wqkv_t); dev_free(l.wo_t); dev_free(l.wgu_t); dev_free(l.wd_t); dev_free(l.g_attn); dev_free(l.g_ffn);
+            dev_free(l.qk_gains);
         }
         dev_free(c->rope_cs);
         dev_free(c->pool);
@@ -486,6 +335,7 @@ extern "C" ps_status ps_kv_alloc(ps_ctx* c, int32_t n_pages, int32_t n_kv_layers
         HIP_TRY(c, hipMemsetAsync(c->pool, 0, slot_elems * n_kv_layers * 2, c->stream));
         HIP_TRY(c, hipStreamSynchronize(c->stream));
     }
+    c->pool_id++;
     c->n_pool_pages = n_pages;
     c->n_kv_slots = n_kv_layers;
     c->slot_elems = slot_elems;
@@ -696,9 +546,7 @@ extern "C" ps_status ps_set_taps(ps_ctx* c, int32_t layer, const ps_taps* taps) 
 }
 
 // ------------------------------------------------------------------------------ the step
-static size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
-
-static GemmOptions gemm_options(const ps_ctx* c) {
+GemmOptions ps::gemm_options(const ps_ctx* c) {
     GemmOptions o;
     o.split_k = c->opt_gemm_split_k; o.tile = c->opt_gemm_tile; o.sk_mode = c->opt_gemm_whole_tiles;
     o.wreg = c->opt_gemm_wreg;
@@ -706,14 +554,14 @@ static GemmOptions gemm_options(const ps_ctx* c) {
     return o;
 }
 // The output projection of the model writes one partial buffer: it is the logits.
-static GemmOptions head_options(const ps_ctx* c) {
+GemmOptions ps::head_options(const ps_ctx* c) {
     GemmOptions o = gemm_options(c);
     o.split_k = 1;
     return o;
 }
 
 // Memory of a step's projections.
-static LayerNeeds layer_needs(const ps_ctx* c, int T, const GemmOptions& o) {
+LayerNeeds ps::layer_needs(const ps_ctx* c, int T, const GemmOptions& o) {
     const ps_model_desc& d = c->desc;
     const int H = d.hidden, F = d.ffn, NQ = d.n_q_heads * d.head_dim;
     const int shapes[4][3] = {{qkv_cols(d), H, GemmOut::PARTIAL_F32}, {H, NQ, GemmOut::PARTIAL_F32}, {2 * F, H, GemmOut::SWIGLU_BF16}, {H, F, GemmOut::PARTIAL_F32}};
@@ -728,7 +576,7 @@ static LayerNeeds layer_needs(const ps_ctx* c, int T, const GemmOptions& o) {
     return n;
 }
 
-static ps_status ensure_workspaces(ps_ctx* c, int T, int n_part_slots, int head_rows, const LayerNeeds& needs, const GemmOptions& o) {
+ps_status ps::ensure_workspaces(ps_ctx* c, int T, int n_part_slots, int head_rows, const LayerNeeds& needs, const GemmOptions& o) {
     const ps_model_desc& d = c->desc;
     if (T > c->cap_tokens) {
         HIP_TRY(c, hipStreamSynchronize(c->stream));
@@ -803,6 +651,26 @@ static ps_status ensure_workspaces(ps_ctx* c, int T, int n_part_slots, int head_
     return PS_OK;
 }
 
+// The output projection's result where the caller takes none.
+ps_status ps::ensure_logits(ps_ctx* c, size_t bytes) {
+    if (bytes <= c->logits_bytes) return PS_OK;
+    HIP_TRY(c, hipStreamSynchronize(c->stream));
+    dev_free(c->ws_logits);
+    c->logits_bytes = 0;
+    ps_status st = dev_alloc(c, &c->ws_logits, bytes + bytes / 4, "logits");
+    if (st == PS_OK) c->logits_bytes = bytes + bytes / 4;
+    return st;
+}
+
+StepBufs ps::workspace_bufs(ps_ctx* c, const GemmOptions& o) {
+    StepBufs W;
+    W.gemm = o;
+    W.xn = c->ws_xn; W.q = c->ws_q; W.attn = c->ws_attn; W.act = c->ws_act; W.x1 = c->ws_x1; W.xmid = c->ws_xmid;
+    W.part = c->ws_part; W.part_o = c->part_o; W.part_ml = c->part_ml; W.part_bytes = c->part_bytes; W.act_bytes = c->act_bytes;
+    W.skfrag = c->ws_skfrag; W.skfrag_bytes = c->skfrag_bytes; W.skcnt = c->ws_skcnt; W.skcnt_n = c->skcnt_n;
+    return W;
+}
+
 struct MetaLayout {
     size_t positions, slots, seqs, pages, items, workers, groups, tokens, last_rows, total;
 };
@@ -830,20 +698,6 @@ struct TokenIO {
     float* logits;             // device [n_seqs][vocab] or null
     float* hidden;             // device [T][hidden] fp32 or null
     float* ms;                 // host [3] or null: embedding, stack, head (needs stats-style synchronisation)
-};
-
-// Device buffers of one step besides its inputs and outputs: the library's growing workspaces (ps_step,
-// ps_step_tokens) or pieces of the static scratch array (ps_step_static).
-struct StepBufs {
-    bf16_t *xn = nullptr, *q = nullptr, *attn = nullptr, *act = nullptr;
-    float *x1 = nullptr, *xmid = nullptr, *part = nullptr, *part_o = nullptr, *part_ml = nullptr;
-    size_t part_bytes = 0, act_bytes = 0;
-    float* skfrag = nullptr;
-    size_t skfrag_bytes = 0;
-    int* skcnt = nullptr;
-    int skcnt_n = 0;
-    GemmOptions gemm;      // of the layer projections
-    char* meta = nullptr;  // static steps only: device copy of the metadata
 };
 
 // partials_shared: the attention partials, which live from the attention launch to its merge, lie over what only the projections
@@ -936,6 +790,181 @@ static ps_status carve_static(ps_ctx* c, size_t meta_bytes, StepBufs* w) {
     return PS_OK;
 }
 
+ps_status ps::poison(ps_ctx* c, const StepBufs& W, int T, int n_part_slots) {
+    const ps_model_desc& d = c->desc;
+    const int H = d.hidden, NQ = d.n_q_heads * d.head_dim;
+    // every buffer the step's kernels write before they read: bf16 NaN (0x7FC0) everywhere, which as fp32 words is a
+    // NaN too.  A kernel that reads what no kernel of this step wrote carries it into the output.
+    const uint32_t nan2 = 0x7FC07FC0u;
+    const size_t T16 = (size_t)((T + 15) & ~15);
+    HIP_TRY(c, launch_fill_words(W.xn, T16 * H * 2, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.q, (size_t)T * NQ * 2, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.attn, T16 * NQ * 2, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.act, W.act_bytes, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.x1, (size_t)T * H * 4, nan2, c->stream));
+    if (W.xmid) HIP_TRY(c, launch_fill_words(W.xmid, (size_t)T * H * 4, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.part, W.part_bytes, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.part_o, (size_t)n_part_slots * 16 * d.head_dim * 4, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.part_ml, (size_t)n_part_slots * 16 * 2 * 4, nan2, c->stream));
+    HIP_TRY(c, launch_fill_words(W.skfrag, W.skfrag_bytes, nan2, c->stream));
+    return PS_OK;
+}
+
+// Sizes of the attention launch that the lists of a plan are for.
+void ps::set_work_lists(const StepPlan& p, const ps_model_desc& d, AttnArgs* a) {
+    a->n_items = (int)p.items.size();
+    a->n_workers = (int)p.worker_begin.size() - 1;
+    a->n_team = p.n_team_workers;
+    a->n_groups = (int)p.groups.size();
+    a->max_splits = 0;
+    a->max_merge_rows = 0;
+    for (const MergeGroup& mg : p.groups) {
+        a->max_splits = std::max(a->max_splits, (int)mg.n_splits);
+        a->max_merge_rows = std::max(a->max_merge_rows, (int)mg.n_tok * (d.n_q_heads / d.n_kv_heads));
+    }
+    a->n_q = d.n_q_heads; a->n_kv = d.n_kv_heads; a->d = d.head_dim;
+}
+
+// The layers, one after another.
+ps_status ps::run_stack(ps_ctx* c, const StackRun& r) {
+    const ps_model_desc& d = c->desc;
+    const int T = r.T, H = d.hidden, F = d.ffn, NQ = d.n_q_heads * d.head_dim, NQKV = qkv_cols(d);
+    const StepBufs& W = *r.bufs;
+    ps_step_stats* const stats = r.stats;
+    const void* const x_in = r.x_in;
+    void* const x_out = r.x_out;
+    const bool out_f32 = r.out_f32;
+    if (stats && !c->have_events) {
+        for (auto& e : c->ev) HIP_TRY(c, hipEventCreate(&e));
+        c->have_events = true;
+    }
+    // with stats, events bracket every stage of every layer; stage times are summed over layers
+    std::vector<float> stage_ms(PS_N_STAGES, 0.f);
+    float total_ms = 0.f;
+    hipStream_t s = c->stream;
+
+    // The residual stream stays fp32 inside the stack: only x_in and x_out are bf16.  Every
+    // projection leaves fp32 partial sums; the kernel that consumes them adds them up.
+    const void* x_cur = x_in;
+    bool x_cur_f32 = false;
+    // only_layer: the step runs that one layer as a whole model (x_in -> x_out)
+    const int l_begin = c->opt_only_layer >= 0 ? c->opt_only_layer : 0;
+    const int l_end = c->opt_only_layer >= 0 ? c->opt_only_layer + 1 : d.n_layers;
+    for (int l = l_begin; l < l_end; l++) {
+        const LayerWeights& L = c->layers[l];
+        const bool tap = (l == c->tap_layer);
+        const bool last = (l == l_end - 1);
+        bf16_t* pool_slot = c->pool + (size_t)(l % c->n_kv_slots) * c->slot_elems;
+        int e = 0, n_splits = 1;
+        // event pairs around this layer's four projection launches, when asked for and while the ring has room
+        hipEvent_t* gev = nullptr;
+        if (c->opt_time_gemm > 0 && c->gemm_ev_count < GEMM_EV_RECS && (c->step_counter % c->opt_time_gemm) == 0)
+            gev = c->gemm_ev.data() + (size_t)8 * c->gemm_ev_count++;
+        auto run_gemm = [&](const GemmArgs& ga, int* splits, int which) -> hipError_t {
+            if (gev) (void)hipEventRecord(gev[2 * which], s);
+            const hipError_t ge = launch_gemm(ga, splits, s);
+            if (gev) (void)hipEventRecord(gev[2 * which + 1], s);
+            return ge;
+        };
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[e], s));
+        // 0: RMSNorm of the layer input (layers after the first get it from the previous layer's last kernel)
+        if (l == l_begin) HIP_TRY(c, launch_rmsnorm(x_cur, x_cur_f32, L.g_attn, W.xn, T, H, d.rms_eps, s, nullptr, r.fetch_src, r.fetch_dst, r.fetch_bytes));
+        if (tap && c->taps.xn) HIP_TRY(c, launch_untile(W.xn, static_cast<bf16_t*>(c->taps.xn), T, H, s));
+        if (tap && c->taps.x_in && l > l_begin) HIP_TRY(c, launch_copy_bytes(x_cur, c->taps.x_in, (size_t)T * H * 4, s));
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+        // 1: QKV projection -> fp32 partials
+        GemmArgs g{};
+        g.A = W.xn; g.Wp = L.wqkv_t; g.M = T; g.N = NQKV; g.K = H; g.kind = GemmOut::PARTIAL_F32;
+        g.out = W.part; g.out_bytes = W.part_bytes; g.opt = W.gemm;
+        g.sk_frag = W.skfrag; g.sk_frag_bytes = W.skfrag_bytes; g.sk_counters = W.skcnt; g.sk_n_counters = W.skcnt_n;
+        const RopeOut rope{W.q, pool_slot, r.positions, r.slots, reinterpret_cast<const float2*>(c->rope_cs), d.n_q_heads, d.n_kv_heads, d.head_dim};
+        if (!L.qk_norm) g.rope = rope;   // a normalised head has to be whole before it is rotated
+        HIP_TRY(c, run_gemm(g, &n_splits, 0));
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+        // 2: sum the partials, rotate, round once to bf16, append k/v to the pages
+        if (L.qk_norm)
+            HIP_TRY(c, launch_qk_norm_rope(NormRopeArgs{W.part, false, n_splits, (size_t)T * NQKV, NQKV, rope, L.qk_gains, d.rms_eps, T}, s));
+        else if (n_splits > 0)
+            HIP_TRY(c, launch_rope_append(W.part, n_splits, rope, T, s));   // 0: the GEMM has done it
+        g.rope = RopeOut{};
+        if (tap && c->taps.q) HIP_TRY(c, launch_copy_bytes(W.q, c->taps.q, (size_t)T * NQ * 2, s));
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+        // 3: attention
+        AttnArgs a = r.tree ? static_cast<const AttnArgs&>(*r.tree) : *r.attn;
+        a.q = W.q; a.ldq = NQ; a.pool_slot = pool_slot; a.out = W.attn;
+        if (!r.tree) { a.part_o = W.part_o; a.part_ml = W.part_ml; }
+        const bool time_attn = c->opt_time_attention > 0 && c->attn_ev_count < ATTN_EV_PAIRS &&
+                               (c->step_counter % c->opt_time_attention) == 0;
+        a.ev_begin = time_attn ? c->attn_ev[2 * c->attn_ev_count] : nullptr;
+        a.ev_end = time_attn ? c->attn_ev[2 * c->attn_ev_count + 1] : nullptr;
+        if (r.tree) {
+            TreeArgs ta = *r.tree;
+            static_cast<AttnArgs&>(ta) = a;
+            HIP_TRY(c, launch_tree_attention(ta, s));
+        } else {
+            HIP_TRY(c, launch_attention(a, s));
+        }
+        if (time_attn) c->attn_ev_count++;
+        if (tap && c->taps.attn) HIP_TRY(c, launch_untile(W.attn, static_cast<bf16_t*>(c->taps.attn), T, NQ, s));
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+        // 4: O projection -> fp32 partials
+        g.A = W.attn; g.Wp = L.wo_t; g.N = H; g.K = NQ;
+        HIP_TRY(c, run_gemm(g, &n_splits, 1));
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+        // 5: x1 = x + sum(partials) (fp32), xn = RMSNorm(x1)
+        ReduceAddNormArgs ra{};
+        ra.resid = x_cur; ra.resid_f32 = x_cur_f32; ra.partials = W.part; ra.n_splits = n_splits; ra.T = T; ra.H = H;
+        ra.x_f32 = W.x1; ra.x_bf16 = nullptr; ra.gain = L.g_ffn; ra.xn = W.xn; ra.eps = d.rms_eps;
+        HIP_TRY(c, launch_reduce_add_norm(ra, s));
+        if (tap && c->taps.x1) HIP_TRY(c, launch_copy_bytes(W.x1, c->taps.x1, (size_t)T * H * 4, s));
+        if (tap && c->taps.xn2) HIP_TRY(c, launch_untile(W.xn, static_cast<bf16_t*>(c->taps.xn2), T, H, s));
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+        // 6: gate/up + SwiGLU
+        g.A = W.xn; g.Wp = L.wgu_t; g.N = 2 * F; g.K = H; g.kind = GemmOut::SWIGLU_BF16;
+        g.out = W.act; g.out_bytes = W.act_bytes;
+        HIP_TRY(c, run_gemm(g, nullptr, 2));
+        if (tap && c->taps.act) HIP_TRY(c, launch_untile(W.act, static_cast<bf16_t*>(c->taps.act), T, F, s));
+        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+        // 7: down projection -> fp32 partials; out = x1 + sum(partials); for an inner layer also the
+        //    next layer's normalised input
+        g.A = W.act; g.Wp = L.wd_t; g.N = H; g.K = F; g.kind = GemmOut::PARTIAL_F32;
+        g.out = W.part; g.out_bytes = W.part_bytes;
+        HIP_TRY(c, run_gemm(g, &n_splits, 3));
+        ra.resid = W.x1; ra.resid_f32 = true; ra.n_splits = n_splits;
+        if (last) {
+            ra.x_f32 = out_f32 ? static_cast<float*>(x_out) : nullptr;
+            ra.x_bf16 = out_f32 ? nullptr : static_cast<bf16_t*>(x_out);
+            ra.gain = nullptr; ra.xn = nullptr;
+        } else {
+            ra.x_f32 = W.xmid; ra.x_bf16 = nullptr;
+            ra.gain = c->layers[l + 1].g_attn; ra.xn = W.xn;
+        }
+        HIP_TRY(c, launch_reduce_add_norm(ra, s));
+        void* x_next = last ? x_out : static_cast<void*>(W.xmid);
+        if (tap && c->taps.x_out && (!last || out_f32))
+            HIP_TRY(c, launch_copy_bytes(x_next, c->taps.x_out, (size_t)T * H * 4, s));
+        if (stats) {
+            HIP_TRY(c, hipEventRecord(c->ev[++e], s));
+            HIP_TRY(c, hipEventSynchronize(c->ev[e]));
+            for (int i = 0; i < PS_N_STAGES; i++) {
+                float ms = 0.f;
+                HIP_TRY(c, hipEventElapsedTime(&ms, c->ev[i], c->ev[i + 1]));
+                stage_ms[i] += ms;
+            }
+            float ms = 0.f;
+            HIP_TRY(c, hipEventElapsedTime(&ms, c->ev[0], c->ev[PS_N_STAGES]));
+            total_ms += ms;
+        }
+        x_cur = x_next;
+        x_cur_f32 = true;
+    }
+    if (stats) {
+        stats->ms_total = total_ms;
+        for (int i = 0; i < PS_N_STAGES; i++) stats->ms_stage[i] = stage_ms[i];
+    }
+    return PS_OK;
+}
+
 static ps_status step_impl(ps_ctx* c, const ps_seq* seqs, int32_t n_seqs, const void* x_in, void* x_out, ps_step_stats* stats,
                            const TokenIO* tio, bool use_static = false) {
     if (!c) return PS_EINVAL;
@@ -971,7 +1000,7 @@ static ps_status step_impl(ps_ctx* c, const ps_seq* seqs, int32_t n_seqs, const 
 
     c->step_counter++;
     const ps_model_desc& d = c->desc;
-    const int T = p.n_tokens, H = d.hidden, F = d.ffn, NQ = d.n_q_heads * d.head_dim, NQKV = qkv_cols(d);
+    const int T = p.n_tokens, H = d.hidden;
     const MetaLayout ml = meta_layout(p, tio != nullptr);
     StepBufs W;
     W.gemm = c->memory.gemm;
@@ -979,25 +1008,10 @@ static ps_status step_impl(ps_ctx* c, const ps_seq* seqs, int32_t n_seqs, const 
         if ((st = carve_static(c, ml.total, &W)) != PS_OK) return st;
     } else {
         if ((st = ensure_workspaces(c, T, p.n_partial_slots, tio ? p.n_seqs : 0, c->memory.needs, W.gemm)) != PS_OK) return st;
-        W.xn = c->ws_xn; W.q = c->ws_q; W.attn = c->ws_attn; W.act = c->ws_act; W.x1 = c->ws_x1; W.xmid = c->ws_xmid;
-        W.part = c->ws_part; W.part_o = c->part_o; W.part_ml = c->part_ml; W.part_bytes = c->part_bytes; W.act_bytes = c->act_bytes;
-        W.skfrag = c->ws_skfrag; W.skfrag_bytes = c->skfrag_bytes; W.skcnt = c->ws_skcnt; W.skcnt_n = c->skcnt_n;
+        W = workspace_bufs(c, c->memory.gemm);
     }
     if (c->opt_poison) {
-        // every buffer the step's kernels write before they read: bf16 NaN (0x7FC0) everywhere, which as fp32 words is a
-        // NaN too.  A kernel that reads what no kernel of this step wrote carries it into the output.
-        const uint32_t nan2 = 0x7FC07FC0u;
-        const size_t T16 = (size_t)((T + 15) & ~15);
-        HIP_TRY(c, launch_fill_words(W.xn, T16 * H * 2, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.q, (size_t)T * NQ * 2, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.attn, T16 * NQ * 2, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.act, W.act_bytes, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.x1, (size_t)T * H * 4, nan2, c->stream));
-        if (W.xmid) HIP_TRY(c, launch_fill_words(W.xmid, (size_t)T * H * 4, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.part, W.part_bytes, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.part_o, (size_t)p.n_partial_slots * 16 * d.head_dim * 4, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.part_ml, (size_t)p.n_partial_slots * 16 * 2 * 4, nan2, c->stream));
-        HIP_TRY(c, launch_fill_words(W.skfrag, W.skfrag_bytes, nan2, c->stream));
+        if ((st = poison(c, W, T, p.n_partial_slots)) != PS_OK) return st;
     }
     // the array of a static step keeps whatever the previous call left where this call's tile counters lie
     if (use_static && W.skcnt_n > 0) HIP_TRY(c, launch_fill_zero(W.skcnt, (size_t)W.skcnt_n * sizeof(int), c->stream));
@@ -1050,13 +1064,6 @@ static ps_status step_impl(ps_ctx* c, const ps_seq* seqs, int32_t n_seqs, const 
     const int32_t* d_pos = reinterpret_cast<const int32_t*>(db + ml.positions);
     const int32_t* d_slots = reinterpret_cast<const int32_t*>(db + ml.slots);
 
-    if (stats && !c->have_events) {
-        for (auto& e : c->ev) HIP_TRY(c, hipEventCreate(&e));
-        c->have_events = true;
-    }
-    // with stats, events bracket every stage of every layer; stage times are summed over layers
-    std::vector<float> stage_ms(PS_N_STAGES, 0.f);
-    float total_ms = 0.f;
     hipStream_t s = c->stream;
 
     // Full-model step: the stack's input is the embedding rows of the step's tokens, its output stays fp32
@@ -1070,145 +1077,22 @@ static ps_status step_impl(ps_ctx* c, const ps_seq* seqs, int32_t n_seqs, const 
         x_in = c->ws_embed;
         x_out = tio->hidden ? static_cast<void*>(tio->hidden) : static_cast<void*>(c->ws_final);
     }
-    // The residual stream stays fp32 inside the stack: only x_in and x_out are bf16.  Every
-    // projection leaves fp32 partial sums; the kernel that consumes them adds them up.
-    const void* x_cur = x_in;
-    bool x_cur_f32 = false;
-    // only_layer: the step runs that one layer as a whole model (x_in -> x_out)
-    const int l_begin = c->opt_only_layer >= 0 ? c->opt_only_layer : 0;
-    const int l_end = c->opt_only_layer >= 0 ? c->opt_only_layer + 1 : d.n_layers;
-    for (int l = l_begin; l < l_end; l++) {
-        const LayerWeights& L = c->layers[l];
-        const bool tap = (l == c->tap_layer);
-        const bool last = (l == l_end - 1);
-        bf16_t* pool_slot = c->pool + (size_t)(l % c->n_kv_slots) * c->slot_elems;
-        int e = 0, n_splits = 1;
-        // event pairs around this layer's four projection launches, when asked for and while the ring has room
-        hipEvent_t* gev = nullptr;
-        if (c->opt_time_gemm > 0 && c->gemm_ev_count < GEMM_EV_RECS && (c->step_counter % c->opt_time_gemm) == 0)
-            gev = c->gemm_ev.data() + (size_t)8 * c->gemm_ev_count++;
-        auto run_gemm = [&](const GemmArgs& ga, int* splits, int which) -> hipError_t {
-            if (gev) (void)hipEventRecord(gev[2 * which], s);
-            const hipError_t ge = launch_gemm(ga, splits, s);
-            if (gev) (void)hipEventRecord(gev[2 * which + 1], s);
-            return ge;
-        };
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[e], s));
-        // 0: RMSNorm of the layer input (layers after the first get it from the previous layer's last kernel)
-        if (l == l_begin) HIP_TRY(c, launch_rmsnorm(x_cur, x_cur_f32, L.g_attn, W.xn, T, H, d.rms_eps, s, nullptr, fetch_src, fetch_dst, fetch_src ? ml.total : 0));
-        if (tap && c->taps.xn) HIP_TRY(c, launch_untile(W.xn, static_cast<bf16_t*>(c->taps.xn), T, H, s));
-        if (tap && c->taps.x_in && l > l_begin) HIP_TRY(c, launch_copy_bytes(x_cur, c->taps.x_in, (size_t)T * H * 4, s));
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-        // 1: QKV projection -> fp32 partials
-        GemmArgs g{};
-        g.A = W.xn; g.Wp = L.wqkv_t; g.M = T; g.N = NQKV; g.K = H; g.kind = GemmOut::PARTIAL_F32;
-        g.out = W.part; g.out_bytes = W.part_bytes; g.opt = W.gemm;
-        g.sk_frag = W.skfrag; g.sk_frag_bytes = W.skfrag_bytes; g.sk_counters = W.skcnt; g.sk_n_counters = W.skcnt_n;
-        g.rope = RopeOut{W.q, pool_slot, d_pos, d_slots, reinterpret_cast<const float2*>(c->rope_cs), d.n_q_heads, d.n_kv_heads, d.head_dim};
-        HIP_TRY(c, run_gemm(g, &n_splits, 0));
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-        // 2: sum the partials, rotate, round once to bf16, append k/v to the pages
-        if (n_splits > 0) HIP_TRY(c, launch_rope_append(W.part, n_splits, g.rope, T, s));   // 0: the GEMM has done it
-        g.rope = RopeOut{};
-        if (tap && c->taps.q) HIP_TRY(c, launch_copy_bytes(W.q, c->taps.q, (size_t)T * NQ * 2, s));
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-        // 3: attention
-        AttnArgs a{};
-        a.q = W.q; a.ldq = NQ; a.pool_slot = pool_slot;
-        a.seqs = reinterpret_cast<const SeqInfo*>(db + ml.seqs);
-        a.pages = reinterpret_cast<const int32_t*>(db + ml.pages);
-        a.items = reinterpret_cast<const AttnItem*>(db + ml.items);
-        a.n_items = (int)p.items.size();
-        a.worker_begin = reinterpret_cast<const int32_t*>(db + ml.workers);
-        a.n_workers = (int)p.worker_begin.size() - 1;
-        a.n_team = p.n_team_workers;
-        a.groups = reinterpret_cast<const MergeGroup*>(db + ml.groups);
-        a.n_groups = (int)p.groups.size();
-        a.max_splits = 0;
-        a.max_merge_rows = 0;
-        for (const MergeGroup& mg : p.groups) {
-            a.max_splits = std::max(a.max_splits, (int)mg.n_splits);
-            a.max_merge_rows = std::max(a.max_merge_rows, (int)mg.n_tok * (d.n_q_heads / d.n_kv_heads));
-        }
-        a.part_o = W.part_o; a.part_ml = W.part_ml; a.out = W.attn;
-        a.n_q = d.n_q_heads; a.n_kv = d.n_kv_heads; a.d = d.head_dim;
-        const bool time_attn = c->opt_time_attention > 0 && c->attn_ev_count < ATTN_EV_PAIRS &&
-                               (c->step_counter % c->opt_time_attention) == 0;
-        a.ev_begin = time_attn ? c->attn_ev[2 * c->attn_ev_count] : nullptr;
-        a.ev_end = time_attn ? c->attn_ev[2 * c->attn_ev_count + 1] : nullptr;
-        HIP_TRY(c, launch_attention(a, s));
-        if (time_attn) c->attn_ev_count++;
-        if (tap && c->taps.attn) HIP_TRY(c, launch_untile(W.attn, static_cast<bf16_t*>(c->taps.attn), T, NQ, s));
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-        // 4: O projection -> fp32 partials
-        g.A = W.attn; g.Wp = L.wo_t; g.N = H; g.K = NQ;
-        HIP_TRY(c, run_gemm(g, &n_splits, 1));
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-        // 5: x1 = x + sum(partials) (fp32), xn = RMSNorm(x1)
-        ReduceAddNormArgs r{};
-        r.resid = x_cur; r.resid_f32 = x_cur_f32; r.partials = W.part; r.n_splits = n_splits; r.T = T; r.H = H;
-        r.x_f32 = W.x1; r.x_bf16 = nullptr; r.gain = L.g_ffn; r.xn = W.xn; r.eps = d.rms_eps;
-        HIP_TRY(c, launch_reduce_add_norm(r, s));
-        if (tap && c->taps.x1) HIP_TRY(c, launch_copy_bytes(W.x1, c->taps.x1, (size_t)T * H * 4, s));
-        if (tap && c->taps.xn2) HIP_TRY(c, launch_untile(W.xn, static_cast<bf16_t*>(c->taps.xn2), T, H, s));
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-        // 6: gate/up + SwiGLU
-        g.A = W.xn; g.Wp = L.wgu_t; g.N = 2 * F; g.K = H; g.kind = GemmOut::SWIGLU_BF16;
-        g.out = W.act; g.out_bytes = W.act_bytes;
-        HIP_TRY(c, run_gemm(g, nullptr, 2));
-        if (tap && c->taps.act) HIP_TRY(c, launch_untile(W.act, static_cast<bf16_t*>(c->taps.act), T, F, s));
-        if (stats) HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-        // 7: down projection -> fp32 partials; out = x1 + sum(partials); for an inner layer also the
-        //    next layer's normalised input
-        g.A = W.act; g.Wp = L.wd_t; g.N = H; g.K = F; g.kind = GemmOut::PARTIAL_F32;
-        g.out = W.part; g.out_bytes = W.part_bytes;
-        HIP_TRY(c, run_gemm(g, &n_splits, 3));
-        r.resid = W.x1; r.resid_f32 = true; r.n_splits = n_splits;
-        if (last) {
-            r.x_f32 = out_f32 ? static_cast<float*>(x_out) : nullptr;
-            r.x_bf16 = out_f32 ? nullptr : static_cast<bf16_t*>(x_out);
-            r.gain = nullptr; r.xn = nullptr;
-        } else {
-            r.x_f32 = W.xmid; r.x_bf16 = nullptr;
-            r.gain = c->layers[l + 1].g_attn; r.xn = W.xn;
-        }
-        HIP_TRY(c, launch_reduce_add_norm(r, s));
-        void* x_next = last ? x_out : static_cast<void*>(W.xmid);
-        if (tap && c->taps.x_out && (!last || out_f32))
-            HIP_TRY(c, launch_copy_bytes(x_next, c->taps.x_out, (size_t)T * H * 4, s));
-        if (stats) {
-            HIP_TRY(c, hipEventRecord(c->ev[++e], s));
-            HIP_TRY(c, hipEventSynchronize(c->ev[e]));
-            for (int i = 0; i < PS_N_STAGES; i++) {
-                float ms = 0.f;
-                HIP_TRY(c, hipEventElapsedTime(&ms, c->ev[i], c->ev[i + 1]));
-                stage_ms[i] += ms;
-            }
-            float ms = 0.f;
-            HIP_TRY(c, hipEventElapsedTime(&ms, c->ev[0], c->ev[PS_N_STAGES]));
-            total_ms += ms;
-        }
-        x_cur = x_next;
-        x_cur_f32 = true;
-    }
-    if (stats) {
-        stats->ms_total = total_ms;
-        for (int i = 0; i < PS_N_STAGES; i++) stats->ms_stage[i] = stage_ms[i];
-    }
+    AttnArgs a{};
+    a.seqs = reinterpret_cast<const SeqInfo*>(db + ml.seqs);
+    a.pages = reinterpret_cast<const int32_t*>(db + ml.pages);
+    a.items = reinterpret_cast<const AttnItem*>(db + ml.items);
+    a.worker_begin = reinterpret_cast<const int32_t*>(db + ml.workers);
+    a.groups = reinterpret_cast<const MergeGroup*>(db + ml.groups);
+    set_work_lists(p, c->desc, &a);
+    const StackRun run{&W, T, d_pos, d_slots, &a, nullptr, fetch_src, fetch_dst, fetch_src ? ml.total : 0, x_in, x_out, out_f32, stats};
+    if ((st = run_stack(c, run)) != PS_OK) return st;
     if (tio) {
         // head: RMS normalisation of every sequence's last new token, output projection, greedy token
         if (tio->ms) HIP_TRY(c, hipEventRecord(c->ev_head[2], s));
         const int M = p.n_seqs, V = c->vocab;
         float* logits = tio->logits;
         if (!logits) {
-            const size_t need = (size_t)M * V * sizeof(float);
-            if (need > c->logits_bytes) {
-                HIP_TRY(c, hipStreamSynchronize(s));
-                dev_free(c->ws_logits);
-                c->logits_bytes = 0;
-                if ((st = dev_alloc(c, &c->ws_logits, need + need / 4, "logits")) != PS_OK) return st;
-                c->logits_bytes = need + need / 4;
-            }
+            if ((st = ensure_logits(c, (size_t)M * V * sizeof(float))) != PS_OK) return st;
             logits = c->ws_logits;
         }
         int32_t* next = tio->next_tokens;

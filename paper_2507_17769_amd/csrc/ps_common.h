@@ -57,7 +57,9 @@ struct AttnItem {
     int32_t pos0;        // cache position of that token
     int32_t page_off;    // offset of the sequence's page list in the flat page array
     int32_t page0, page1;  // physical ids of the item's first two pages: the first loads need no table lookup
-    int32_t pad0, pad1, pad2;
+    // Trees only: what a token of the block sees of the sequence's new tokens, one bit a cache position, as mask_words words a token
+    // from word mask_at on (the block's first token); the first word stands for the positions 32 mask_pair on.  mask_at < 0: causal.
+    int32_t mask_at, mask_words, mask_pair;
 };
 
 // Split-KV merge group: one 16-row query tile of one (sequence, kv head).
@@ -173,6 +175,52 @@ struct AttnArgs {
     hipEvent_t ev_begin, ev_end;  // optional: recorded right before / after the main kernel (not the merge)
 };
 hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
+// The same for batches whose new tokens form trees (tree_attention.hip).
+struct TreeArgs : AttnArgs {
+    const uint32_t* masks;   // see AttnItem
+    int nt;                  // 16-row tiles of a team's wavefront
+    int64_t ldo;             // row stride of out in elements; 0: operand order
+};
+hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t st);
+int tree_tokens_per_item(int G, int nt);   // of a team with nt tiles to a wavefront
+
+// Normalise the heads of queries and keys, rotate, append (qk_norm.hip).
+struct NormRopeArgs {
+    const void* qkv;         // [n_splits][T] rows of n_q + 2 n_kv heads
+    bool bf16;               // else fp32
+    int n_splits;            // partial sums to add up, 1 .. 8 (1 for bf16)
+    size_t split_stride;     // elements from one partial sum to the next
+    int64_t ld;              // row stride in elements
+    RopeOut out;
+    const bf16_t* gains;     // [2][d]: queries, keys; null: rotation only
+    float eps;
+    int T;
+};
+hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t st);
+
+// Move cache rows of sequences in all KV slots (tree_keep.hip): sequence i's positions prefix + node (its nodes at [begin[i], begin[i + 1])
+// of node, ascending) to prefix + first[i], prefix + first[i] + 1, ...; first[i] <= its first node.  Host arrays, read before the call returns.
+struct KeepList {
+    int n_seqs;
+    const int32_t *seq, *first, *begin, *node;   // seq: index into seqs
+};
+hipError_t launch_tree_keep(const KeepList& l, bf16_t* pool, size_t slot_elems, int n_slots, const SeqInfo* seqs, const int32_t* pages, int n_kv, int d,
+                            hipStream_t st);
+
+// Rules on logits and the pick (pick.hip); what they mean: ps_logit_rules.
+struct PickArgs {
+    const void* logits;
+    bool bf16;
+    int64_t ld;
+    int n_rows, vocab;
+    ps_logit_rules rules;    // n_lists 0: none
+    float* out;              // or null
+    int64_t ldo;
+    int32_t* next;           // or null
+    float* logprob;          // or null
+};
+hipError_t launch_pick(const PickArgs& a, hipStream_t st);
+
 int attention_worker_slots();  // wavefronts of the attention kernel that are resident at once on this device
 
 }  // namespace ps

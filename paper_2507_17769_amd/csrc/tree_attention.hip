@@ -1,0 +1,585 @@
+// Attention of token trees over the paged cache: every new token ("node") of a sequence attends to the cached prefix, to its
+// ancestors among the new tokens and to itself.
+//
+//     A(i) = {0 .. prefix - 1} + {prefix + j : j = i or an ancestor of i},   out_i = sum_{p in A(i)} softmax(q_i . k_p / sqrt(d)) v_p
+//
+// Parents come before their children, so A(i) lies within the causal range of place i and a batch is planned as a step's chunks
+// and decodes are (planner.cpp): query blocks of several 16-row tiles go to teams of four wavefronts that share pairs of pages
+// through a ring in LDS, single-tile blocks to streaming wavefronts.  What is new is who sees what: the pairs that reach past
+// the prefix, the last few of a stream, are masked by one bit per row and position, read as a word per row and pair; the pairs of
+// the prefix, all others, need no mask.  The two are loops of their own, so the long one carries nothing of the short one.
+//
+// A masked place may hold anything, infinities and NaN too (a rejected branch of an overflowed draft; a page's tail that nobody
+// wrote): its score is replaced, and its value must not reach a row that does not see it, which a zero weight alone does not
+// give (0 * inf is NaN).  In the masked pairs non-finite values are taken out of the product, and where there are any, what
+// the rows that do see them get is counted with three more products (see pv_masked).
+#include "attention_device.h"
+
+#include <algorithm>
+
+namespace ps {
+
+constexpr int TREE_WAVES = 4;
+constexpr int TREE_RING = 3;   // pairs of pages in LDS: the one in use, and two on their way
+
+// What the row of token `qc` of the item's block sees of the 32 positions 32 pair .. 32 pair + 31.
+__device__ __forceinline__ uint32_t visible_word(const TreeArgs& a, const AttnItem& it, int qc, int pair) {
+    if (it.mask_at >= 0) return a.masks[it.mask_at + qc * it.mask_words + (pair - it.mask_pair)];
+    const int left = it.pos0 + qc - 32 * pair;
+    return left >= 31 ? 0xFFFFFFFFu : left < 0 ? 0u : (2u << left) - 1u;
+}
+// Padding sees nothing, not even itself.
+__device__ __forceinline__ bool is_padding(const TreeArgs& a, const AttnItem& it, int qc) {
+    if (it.mask_at < 0) return false;
+    const int p = it.pos0 + qc;
+    return ((a.masks[it.mask_at + qc * it.mask_words + (p >> 5) - it.mask_pair] >> (p & 31)) & 1u) == 0;
+}
+// First pair that needs a mask for rows whose first token sits at pos_first.
+__device__ __forceinline__ int first_masked_pair(const AttnItem& it, int pos_first) { return it.mask_at >= 0 ? it.mask_pair : (pos_first + 1) >> 5; }
+
+// Classes of the eight bf16 values of an operand: 1.0 where the value is of the class.
+enum { POS_INF, NEG_INF, NOT_A_NUMBER };
+__device__ __forceinline__ uint32_t half_class(uint32_t h, int cls) {
+    const bool special = (h & 0x7F80u) == 0x7F80u, nan = (h & 0x7Fu) != 0;
+    const bool hit = special && (cls == NOT_A_NUMBER ? nan : !nan && ((h >> 15) & 1u) == (cls == NEG_INF ? 1u : 0u));
+    return hit ? 0x3F80u : 0u;
+}
+__device__ __forceinline__ u32x4_t class_of(u32x4_t v, int cls) {
+    u32x4_t o;
+#pragma unroll
+    for (int i = 0; i < 4; i++) o[i] = half_class(v[i] & 0xFFFFu, cls) | (half_class(v[i] >> 16, cls) << 16);
+    return o;
+}
+__device__ __forceinline__ u32x4_t without_specials(u32x4_t v) {
+    u32x4_t o;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        o[i] = ((v[i] & 0x7F80u) == 0x7F80u ? 0u : v[i] & 0xFFFFu) | ((v[i] & 0x7F800000u) == 0x7F800000u ? 0u : v[i] & 0xFFFF0000u);
+    return o;
+}
+__device__ __forceinline__ bool has_specials(u32x4_t v) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; i++) any = any || (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
+    return any;
+}
+__device__ __forceinline__ f32x4_t mfma_16x16x32(u32x4_t a, bf16x8_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), b, c, 0, 0, 0);
+}
+
+// o += V^T P^T for one d-tile (16 values of d) of a masked pair.  v: the lane's eight values (d = lane % 16; tokens 4 g .. of either page),
+// seen: ones where the lane's row sees the token.
+__device__ __forceinline__ f32x4_t pv_masked(f32x4_t o, u32x4_t v, bf16x8_t p, bf16x8_t seen) {
+    o = mfma_16x16x32(without_specials(v), p, o);
+    if (__builtin_amdgcn_ballot_w64(has_specials(v)) == 0) return o;
+    const f32x4_t none = {0.f, 0.f, 0.f, 0.f};
+    const f32x4_t up = mfma_16x16x32(class_of(v, POS_INF), seen, none), down = mfma_16x16x32(class_of(v, NEG_INF), seen, none),
+                  nan = mfma_16x16x32(class_of(v, NOT_A_NUMBER), seen, none);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if (up[i] > 0.f) o[i] += __builtin_inff();
+        if (down[i] > 0.f) o[i] -= __builtin_inff();
+        if (nan[i] > 0.f) o[i] = __builtin_nanf("");
+    }
+    return o;
+}
+
+// Scores of the keys that a row does not see become -inf: the running maximum starts at a large finite negative number, so a
+// row that has seen nothing keeps it and gets weights of zero.  word: see visible_word; g: the lane's key group.
+__device__ __forceinline__ bf16x8_t hide(f32x4_t& sa, f32x4_t& sb, uint32_t word, int g) {
+    const uint32_t w = word >> (4 * g);
+    u32x4_t seen;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        sa[i] = (w >> i) & 1u ? sa[i] : -__builtin_inff();
+        sb[i] = (w >> (16 + i)) & 1u ? sb[i] : -__builtin_inff();
+    }
+    seen[0] = (w & 1u ? 0x3F80u : 0u) | (w & 2u ? 0x3F800000u : 0u);
+    seen[1] = (w & 4u ? 0x3F80u : 0u) | (w & 8u ? 0x3F800000u : 0u);
+    seen[2] = (w & 0x10000u ? 0x3F80u : 0u) | (w & 0x20000u ? 0x3F800000u : 0u);
+    seen[3] = (w & 0x40000u ? 0x3F80u : 0u) | (w & 0x80000u ? 0x3F800000u : 0u);
+    return __builtin_bit_cast(bf16x8_t, seen);
+}
+
+// Softmax of one tile for a pair: raw scores -> P as a packed operand, running maximum m (in the scores' units) and the factor
+// alpha of what came before.  The row sums are taken from the rounded P by the matrix unit, so that the weights of a row add up
+// to one exactly as rounded; the maximum is exact, so a row's largest weight carries no rounding.
+__device__ __forceinline__ bf16x8_t tile_softmax(const f32x4_t& sa, const f32x4_t& sb, float& m, float& alpha, float scale2) {
+    const float sv[8] = {sa[0], sa[1], sa[2], sa[3], sb[0], sb[1], sb[2], sb[3]};
+    float mx = max3(max3(sv[0], sv[1], sv[2]), max3(sv[3], sv[4], sv[5]), max3(sv[6], sv[7], m));
+    {
+        const u32x2_t x = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        const float y = max3(__uint_as_float(x.x), __uint_as_float(x.y), mx);
+        const u32x2_t z = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+        mx = max3(__uint_as_float(z.x), __uint_as_float(z.y), y);
+    }
+    const float ms = rounded_product(mx, scale2);
+    alpha = __builtin_amdgcn_exp2f(rounded_product(m, scale2) - ms);
+    m = mx;
+    float pv[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) pv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], scale2, -ms));
+    uint4 pw;
+    pw.x = pack_bf16(pv[0], pv[1]);
+    pw.y = pack_bf16(pv[2], pv[3]);
+    pw.z = pack_bf16(pv[4], pv[5]);
+    pw.w = pack_bf16(pv[6], pv[7]);
+    return as_bf16x8(pw);
+}
+
+// The assembly of max3 reads matrix results: the compiler places no waits for it, so the last product's passes are waited for here.
+__device__ __forceinline__ void matrix_results(f32x4_t& a, f32x4_t& b) { asm volatile("s_nop 15\n\ts_nop 1" : "+v"(a), "+v"(b)); }
+__device__ __forceinline__ void matrix_results(f32x4_t& a, f32x4_t& b, f32x4_t& c, f32x4_t& d) {
+    asm volatile("s_nop 15\n\ts_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+}
+__device__ __forceinline__ void matrix_results(f32x4_t& a, f32x4_t& b, f32x4_t& c, f32x4_t& d, f32x4_t& e, f32x4_t& f) {
+    asm volatile("s_nop 15\n\ts_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d), "+v"(e), "+v"(f));
+}
+
+constexpr u32x4_t ONES = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+
+// What came before is rescaled; once the running maximum has settled alpha is exactly 1 in every lane and nothing is done.
+template <int DT>
+__device__ __forceinline__ void rescale(f32x4_t (&o)[DT], f32x4_t& l, float alpha) {
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) == 0) return;
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) { o[dt][0] *= alpha; o[dt][1] *= alpha; o[dt][2] *= alpha; o[dt][3] *= alpha; }
+    l[0] *= alpha; l[1] *= alpha; l[2] *= alpha; l[3] *= alpha;
+}
+
+// End of an item: the NT tiles of a wavefront go to the output (normalised) or, for an item that covers only part of its KV span, to
+// partial slots it.partial + slot0 + nt.  l: each row's sum, the same in the four lanes that share the row.  Padding gets zeros.
+template <int D, int G, int NT>
+__device__ __forceinline__ void store_rows(const TreeArgs& a, const AttnItem& it, const f32x4_t (&o)[NT][D / 16], const float (&m)[NT], const float (&l)[NT],
+                                           int tok_row, int slot0, int lane) {
+    constexpr int DT = D / 16, TQ = 16 / G;
+    const int r = lane & 15, g = lane >> 4;
+    const int head = it.kv_head * G + (r % G);
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        const int qc = tok_row + nt * TQ;
+        if (qc >= it.q_ntok) continue;   // rows beyond the block's tokens are never merged: do not store them
+        const bool padding = is_padding(a, it, qc);
+        if (it.partial < 0) {
+            const float inv = padding ? 0.f : 1.0f / l[nt];
+            const size_t tok = (size_t)it.tok_g0 + qc;
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) {
+                const int col = head * D + 16 * dt + 4 * g;
+                uint2 w;
+                w.x = padding ? 0u : pack_bf16(o[nt][dt][0] * inv, o[nt][dt][1] * inv);
+                w.y = padding ? 0u : pack_bf16(o[nt][dt][2] * inv, o[nt][dt][3] * inv);
+                *reinterpret_cast<uint2*>(a.out + (a.ldo ? tok * a.ldo + col : act_offset((int)tok, col, a.n_q * D))) = w;
+            }
+        } else {
+            const size_t slot = (size_t)it.partial + slot0 + nt;
+            float* po = a.part_o + (slot * 16 + r) * D + 4 * g;
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++)
+                *reinterpret_cast<float4*>(po + 16 * dt) =
+                    padding ? float4{0.f, 0.f, 0.f, 0.f} : float4{o[nt][dt][0], o[nt][dt][1], o[nt][dt][2], o[nt][dt][3]};
+            if (g == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * 16 + r) * 2) = padding ? float2{NEG_BIG, 0.f} : float2{m[nt], l[nt]};
+        }
+    }
+}
+
+// ---- single-tile blocks: one wavefront -------------------------------------------------------------
+// The next pair of pages is in flight in a second register set while the current one is consumed.
+template <int D, bool MASK>
+__device__ __forceinline__ void wave_pair(f32x4_t (&o)[1][D / 16], f32x4_t& lacc, float& m, const PairRegs<D / 32>& p, const bf16x8_t (&qf)[D / 32],
+                                          uint32_t word, int g, float scale2) {
+    constexpr int KS = D / 32, DT = D / 16;
+    f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+        sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(p.ka[s]), qf[s], sa, 0, 0, 0);
+        sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(p.kb[s]), qf[s], sb, 0, 0, 0);
+    }
+    matrix_results(sa, sb);
+    bf16x8_t seen;
+    if constexpr (MASK) seen = hide(sa, sb, word, g);
+    float alpha;
+    const bf16x8_t pf = tile_softmax(sa, sb, m, alpha, scale2);
+    rescale<DT>(o[0], lacc, alpha);
+    lacc = mfma_16x16x32(ONES, pf, lacc);
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) {
+        const int s = dt >> 1;
+        const u32x4_t v = (dt & 1) ? u32x4_t{p.va[s].z, p.va[s].w, p.vb[s].z, p.vb[s].w} : u32x4_t{p.va[s].x, p.va[s].y, p.vb[s].x, p.vb[s].y};
+        if constexpr (MASK) o[0][dt] = pv_masked(o[0][dt], v, pf, seen);
+        else o[0][dt] = mfma_16x16x32(v, pf, o[0][dt]);
+    }
+}
+
+template <int D, int G>
+__device__ __forceinline__ void wave_item(const TreeArgs& a, const AttnItem it) {
+    constexpr int KS = D / 32, DT = D / 16;
+    const int lane = threadIdx.x & 63;
+    const int r = lane & 15, g = lane >> 4;
+    const int32_t* pages = a.pages + it.page_off;
+    const int head = it.kv_head * G + (r % G);
+    const int qc = min(r / G, it.q_ntok - 1);
+    bf16x8_t qf[KS];
+    const bf16_t* qrow = a.q + (size_t)(it.tok_g0 + qc) * a.ldq + head * D + 8 * g;
+#pragma unroll
+    for (int s = 0; s < KS; s++) qf[s] = as_bf16x8(ldg16(qrow + 32 * s));
+    f32x4_t o[1][DT], lacc = {0.f, 0.f, 0.f, 0.f};
+    float m = NEG_BIG;
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) o[0][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const float scale2 = 1.4426950408889634f / sqrtf((float)D);  // log2(e)/sqrt(d): softmax in base 2
+    const size_t page_stride = (size_t)a.n_kv * 2 * 16 * D;
+    const bf16_t* pool_lane = a.pool_slot + (size_t)it.kv_head * 2 * 16 * D + (size_t)lane * 8;
+
+    const int n_pg = it.page_end - it.page_begin, n_pairs = (n_pg + 1) >> 1, pair0 = it.page_begin >> 1;
+    const int n_free = max(0, min(n_pairs, first_masked_pair(it, it.pos0) - pair0));   // pairs without a mask
+    // page ids 64 at a time, lane l holding page tb0 + l of the item's range
+    int tb0 = 0, tbl = pages[it.page_begin + min(lane, n_pg - 1)];
+    auto load = [&](PairRegs<KS>& p, int i) {   // i < n_pairs
+        if (2 * i >= tb0 + 64) {
+            tb0 += 64;
+            tbl = pages[it.page_begin + tb0 + min(lane, n_pg - tb0 - 1)];
+        }
+        const int la = 2 * i - tb0;
+        load_pair<D>(p, pool_lane, page_stride, __builtin_amdgcn_readlane(tbl, la), __builtin_amdgcn_readlane(tbl, min(la + 1, n_pg - tb0 - 1)));
+    };
+    PairRegs<KS> b0, b1;
+    load(b0, 0);
+    int i = 0;
+    for (; i + 2 <= n_free; i += 2) {
+        load(b1, i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        wave_pair<D, false>(o, lacc, m, b0, qf, 0, g, scale2);
+        __builtin_amdgcn_sched_barrier(0);
+        load(b0, min(i + 2, n_pairs - 1));   // past the last pair: that pair again, not used
+        __builtin_amdgcn_sched_barrier(0);
+        wave_pair<D, false>(o, lacc, m, b1, qf, 0, g, scale2);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // an odd pair of the prefix and the masked pairs, one at a time
+    for (; i < n_pairs; i++) {
+        load(b1, min(i + 1, n_pairs - 1));
+        wave_pair<D, true>(o, lacc, m, b0, qf, i < n_free ? 0xFFFFFFFFu : visible_word(a, it, qc, pair0 + i), g, scale2);
+        b0 = b1;
+    }
+    const float ml[1] = {rounded_product(m, scale2)}, l[1] = {lacc[0]};
+    store_rows<D, G, 1>(a, it, o, ml, l, r / G, 0, lane);
+}
+
+// ---- teams: blocks of several tiles ---------------------------------------------------------------
+// One pair of pages from ring slot `addr` (LDS byte address of this lane's 16 bytes of the slot's first KiB) for the
+// wavefront's NT tiles.  The slot holds the pair as 4 KS KiB blocks [k-step s][K page a, K page b, V page a, V page b].
+template <int D, int NT, bool MASK>
+__device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&lacc)[NT], float (&m)[NT], uint32_t addr, const bf16x8_t (&qf)[NT][D / 32],
+                                          const uint32_t (&word)[NT], int g, float scale2) {
+    constexpr int KS = D / 32, DT = D / 16;
+    u32x4_t kk[2 * KS];
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+        kk[2 * s] = lds_read16(addr, (4 * s + 0) * 1024);
+        kk[2 * s + 1] = lds_read16(addr, (4 * s + 1) * 1024);
+    }
+    if constexpr (KS == 4)
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kk[0]), "+v"(kk[1]), "+v"(kk[2]), "+v"(kk[3]), "+v"(kk[4]), "+v"(kk[5]), "+v"(kk[6]), "+v"(kk[7]));
+    else
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kk[0]), "+v"(kk[1]), "+v"(kk[2]), "+v"(kk[3]));
+    u32x2_t va[DT], vb[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) {
+        va[dt] = lds_read8(addr, (4 * (dt >> 1) + 2) * 1024 + 8 * (dt & 1));
+        vb[dt] = lds_read8(addr, (4 * (dt >> 1) + 3) * 1024 + 8 * (dt & 1));
+    }
+    f32x4_t sa[NT], sb[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        sa[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        sb[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+            sa[nt] = mfma_16x16x32(kk[2 * s], qf[nt][s], sa[nt]);
+            sb[nt] = mfma_16x16x32(kk[2 * s + 1], qf[nt][s], sb[nt]);
+        }
+    }
+    if constexpr (NT == 1) matrix_results(sa[0], sb[0]);
+    else if constexpr (NT == 2) matrix_results(sa[0], sb[0], sa[1], sb[1]);
+    else matrix_results(sa[0], sb[0], sa[1], sb[1], sa[2], sb[2]);
+    bf16x8_t pf[NT], seen[NT];
+    float alpha[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        if constexpr (MASK) seen[nt] = hide(sa[nt], sb[nt], word[nt], g);
+        pf[nt] = tile_softmax(sa[nt], sb[nt], m[nt], alpha[nt], scale2);
+    }
+    if constexpr (DT == 8)
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(va[1]), "+v"(va[2]), "+v"(va[3]), "+v"(va[4]), "+v"(va[5]), "+v"(va[6]), "+v"(va[7]),
+                     "+v"(vb[0]), "+v"(vb[1]), "+v"(vb[2]), "+v"(vb[3]), "+v"(vb[4]), "+v"(vb[5]), "+v"(vb[6]), "+v"(vb[7]));
+    else
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(va[1]), "+v"(va[2]), "+v"(va[3]), "+v"(vb[0]), "+v"(vb[1]), "+v"(vb[2]), "+v"(vb[3]));
+    __builtin_amdgcn_s_setprio(1);   // the matrix unit is fed first (see attn_kernel)
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        rescale<DT>(o[nt], lacc[nt], alpha[nt]);
+        lacc[nt] = mfma_16x16x32(ONES, pf[nt], lacc[nt]);
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) {
+            const u32x4_t v = {va[dt].x, va[dt].y, vb[dt].x, vb[dt].y};
+            if constexpr (MASK) o[nt][dt] = pv_masked(o[nt][dt], v, pf[nt], seen[nt]);
+            else o[nt][dt] = mfma_16x16x32(v, pf[nt], o[nt][dt]);
+        }
+    }
+    __builtin_amdgcn_s_setprio(0);
+}
+
+// One work item on a team.  Wavefront w holds the tiles NT w .. NT w + NT - 1 of the query block and copies the KS KiB blocks
+// w KS .. w KS + KS - 1 of every pair.  Pair i of the item's page range sits in ring slot i % 3.  Per pair: wait for the own copies of
+// this pair (those of the next may still be in flight), barrier (every wavefront's part has landed, and every wavefront has finished
+// with the pair before, whose slot is the one to refill), issue the copies of pair i + 2, compute.  Past the item's last pair the
+// copies fetch that last pair again, into slots nobody reads, so that the wait counts are the same in every trip.
+template <int D, int G, int NT>
+__device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, uint8_t* ring, int wave) {
+    constexpr int KS = D / 32, DT = D / 16, TQ = 16 / G;
+    constexpr int PAIR_BYTES = 4 * KS * 1024;
+    const int lane = threadIdx.x & 63;
+    const int r = lane & 15, g = lane >> 4;
+    const int32_t* pages = a.pages + it.page_off;
+    const int head = it.kv_head * G + (r % G);
+
+    // Row (lane r) of tile nt is token (wave NT + nt) TQ + r / G of the block, clamped to the block's last token (rows past it
+    // compute on that token's data and are not stored).
+    const int tok_row = wave * NT * TQ + r / G;
+    bf16x8_t qf[NT][KS];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        const int qc = min(tok_row + nt * TQ, it.q_ntok - 1);
+        const bf16_t* qrow = a.q + (size_t)(it.tok_g0 + qc) * a.ldq + head * D + 8 * g;
+#pragma unroll
+        for (int s = 0; s < KS; s++) qf[nt][s] = as_bf16x8(ldg16(qrow + 32 * s));
+    }
+    const int wave_tok0 = wave * NT * TQ;
+    const bool wave_has_rows = wave_tok0 < it.q_ntok;
+    const int pos_first = it.pos0 + min(wave_tok0, it.q_ntok - 1);
+    const int pos_last = it.pos0 + min(wave_tok0 + NT * TQ, it.q_ntok) - 1;   // nothing beyond is seen by any row of the wavefront
+
+    f32x4_t o[NT][DT], lacc[NT];
+    float m[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        m[nt] = NEG_BIG;
+        lacc[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) o[nt][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    const float scale2 = 1.4426950408889634f / sqrtf((float)D);
+    const uint32_t page_bytes = (uint32_t)a.n_kv * 2 * 16 * D * 2, lane16 = lane * 16;
+    // block c = wave KS + k of a pair: k-step c / 4, K or V by the second bit of c, page a or b by the first
+    const uint8_t* const pool_wave = reinterpret_cast<const uint8_t*>(a.pool_slot) + (size_t)it.kv_head * 2 * 16 * D * 2 + (wave * KS >> 2) * 1024 +
+                                     (KS == 4 ? 0 : (wave & 1) * 32 * D);
+    const uint32_t ring0 = (uint32_t)(uintptr_t)ring;
+
+    const int n_pg = it.page_end - it.page_begin, n_pairs = (n_pg + 1) >> 1, pair0 = it.page_begin >> 1;
+    int tb0 = 0;   // ids of 64 pages at a time, lane l holding page tb0 + l of the item's range
+    int tbl = pages[it.page_begin + min(lane, n_pg - 1)];
+    auto issue = [&](int j, int slot) {
+        const int jj = min(j, n_pairs - 1);
+        if (2 * jj >= tb0 + 64) {
+            tb0 += 64;
+            tbl = pages[it.page_begin + tb0 + min(lane, n_pg - tb0 - 1)];
+            vm_wait<0>();   // here, so that the compiler does not wait for everything where the paths join
+        }
+        const int la = 2 * jj - tb0;
+        const uint32_t pa = __builtin_amdgcn_readlane(tbl, la);
+        const uint32_t pb = __builtin_amdgcn_readlane(tbl, min(la + 1, n_pg - tb0 - 1));
+        const uint8_t* ca = pool_wave + (uint64_t)pa * page_bytes;
+        const uint8_t* cb = pool_wave + (uint64_t)pb * page_bytes;
+        uint8_t* dst = ring + slot * PAIR_BYTES + wave * (KS * 1024);
+        uint32_t off[2] = {lane16, lane16 + (KS == 4 ? 32 * D : 0)};   // K and V of a page (of head dim 64, a wavefront copies only one)
+        asm volatile("" : "+v"(off[0]), "+v"(off[1]));   // 32-bit offsets in registers of their own: scalar base + vector offset addressing
+#pragma unroll
+        for (int k = 0; k < KS; k++) PS_GLOBAL_TO_LDS(((k & 1) ? cb : ca) + off[k >> 1], dst + k * 1024);
+    };
+
+    __builtin_amdgcn_s_barrier();   // every wavefront has finished with the ring (previous item)
+    issue(0, 0);
+    issue(1, 1);
+    // The wavefront computes on the pairs that begin at or before its last position, first those without a mask, and only keeps copying
+    // and meeting the barriers for the rest: three loops, so that no accumulator is live across a branch.
+    const int n_mine = !wave_has_rows ? 0 : max(0, min(n_pairs, (pos_last >> 5) - pair0 + 1));
+    const int n_free = max(0, min(n_mine, first_masked_pair(it, pos_first) - pair0));
+    int slot = 0;
+    auto step = [&](int i) {
+        vm_wait<KS>();
+        __builtin_amdgcn_s_barrier();
+        issue(i + 2, slot >= 1 ? slot - 1 : TREE_RING - 1);     // (i + 2) % 3
+    };
+    auto next = [&]() { slot = slot + 1 == TREE_RING ? 0 : slot + 1; };
+    uint32_t word[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) word[nt] = 0;
+    int i = 0;
+    for (; i < n_free; i++) {
+        step(i);
+        team_pair<D, NT, false>(o, lacc, m, ring0 + slot * PAIR_BYTES + lane * 16, qf, word, g, scale2);
+        next();
+    }
+    for (; i < n_mine; i++) {
+        step(i);
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) word[nt] = visible_word(a, it, min(tok_row + nt * TQ, it.q_ntok - 1), pair0 + i);
+        team_pair<D, NT, true>(o, lacc, m, ring0 + slot * PAIR_BYTES + lane * 16, qf, word, g, scale2);
+        next();
+    }
+    for (; i < n_pairs; i++) {
+        step(i);
+        next();
+    }
+    vm_wait<0>();   // the surplus copies have landed before the ring is used again
+    if (!wave_has_rows) return;
+    float l[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        l[nt] = lacc[nt][0];
+        m[nt] = rounded_product(m[nt], scale2);   // the merge works in the exponent's units
+    }
+    store_rows<D, G, NT>(a, it, o, m, l, tok_row, wave * NT, lane);
+}
+
+template <int D, int G, int NT>
+__global__ __launch_bounds__(64 * TREE_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_kernel(TreeArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[TREE_RING * (D / 8) * 1024];
+    // contiguous shares of either work list on every XCD, as in attn_kernel
+    const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (j < a.team_per_xcd) {
+        const int t = xcd * a.team_per_xcd + j;
+        if (t >= a.n_team) return;
+        const int i0 = a.worker_begin[t], i1 = a.worker_begin[t + 1];
+        for (int i = i0; i < i1; i++) team_item<D, G, NT>(a, a.items[i], ring, wave);
+    } else {
+        const int w = a.n_team + (xcd * a.wave_blocks_per_xcd + (j - a.team_per_xcd)) * TREE_WAVES + wave;
+        if (j - a.team_per_xcd >= a.wave_blocks_per_xcd || w >= a.n_workers) return;
+        const int i0 = a.worker_begin[w], i1 = a.worker_begin[w + 1];
+        for (int i = i0; i < i1; i++) wave_item<D, G>(a, a.items[i]);
+    }
+}
+
+// Combine split partials of one query tile: out = sum_j 2^(m_j - M) O_j / sum_j 2^(m_j - M) l_j, zeros where no split saw anything.
+// One block per merge group, its wavefronts in a (pass, split) grid as in attn_merge_kernel.
+template <int D, int G>
+__global__ __launch_bounds__(64 * MERGE_MAX_WAVES) void tree_merge_kernel(TreeArgs a) {
+    __shared__ float4 s_acc[MERGE_MAX_WAVES][64];
+    __shared__ float2 s_ml[MERGE_MAX_WAVES][64];
+    const int group = merge_group_of_block(blockIdx.x, a.n_groups);
+    if (group >= a.n_groups) return;
+    const int32_t* gp = reinterpret_cast<const int32_t*>(a.groups + group);
+    MergeGroup mg;
+    mg.tok0 = scalar_read(gp); mg.n_tok = scalar_read(gp + 1); mg.kv_head = scalar_read(gp + 2);
+    mg.first_slot = scalar_read(gp + 3); mg.n_splits = scalar_read(gp + 4); mg.stride = scalar_read(gp + 5);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), NW = blockDim.x >> 6;   // NW: a power of two
+    const int NWS = merge_split_waves(mg.n_splits, NW), NWP = NW / NWS, ws = wave % NWS, wp = wave / NWS;
+    const int n_items = mg.n_tok * G * (D / 4);   // valid rows are the first n_tok * G of the tile
+    for (int c0 = 0; c0 < n_items; c0 += 64 * NWP) {   // the same trip count for every wavefront: the barriers below
+        const int c = c0 + wp * 64 + lane;
+        const bool live = c < n_items;
+        const int r = live ? c / (D / 4) : 0, col = live ? (c % (D / 4)) * 4 : 0;
+        float M = NEG_BIG, L = 0.f;
+        float4 acc = {0.f, 0.f, 0.f, 0.f};
+        const int n_splits = c0 + wp * 64 < n_items ? mg.n_splits : 0;   // a wavefront past the last pass only meets the barriers
+        for (int j0 = ws; j0 < n_splits; j0 += MERGE_BATCH * NWS) {
+            float2 ml[MERGE_BATCH];
+            float4 v[MERGE_BATCH];
+#pragma unroll
+            for (int j = 0; j < MERGE_BATCH; j++)
+                if (j0 + j * NWS < n_splits) {
+                    const size_t row = (size_t)(mg.first_slot + (j0 + j * NWS) * mg.stride) * 16 + r;
+                    ml[j] = *reinterpret_cast<const float2*>(a.part_ml + row * 2);
+                    v[j] = *reinterpret_cast<const float4*>(a.part_o + row * D + col);
+                }
+            float m_new = M;
+#pragma unroll
+            for (int j = 0; j < MERGE_BATCH; j++)
+                if (j0 + j * NWS < n_splits) m_new = fmaxf(m_new, ml[j].x);
+            const float f = __builtin_amdgcn_exp2f(M - m_new);
+            M = m_new;
+            L *= f; acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+#pragma unroll
+            for (int j = 0; j < MERGE_BATCH; j++)
+                if (j0 + j * NWS < n_splits) {
+                    const float w = __builtin_amdgcn_exp2f(ml[j].x - M);
+                    L += w * ml[j].y;
+                    acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
+                }
+        }
+        if (NWS > 1) {
+            s_acc[wave][lane] = acc;
+            s_ml[wave][lane] = float2{M, L};
+            __syncthreads();
+            if (ws == 0) {
+                for (int w = 1; w < NWS; w++) M = fmaxf(M, s_ml[wave + w][lane].x);
+                acc = float4{0.f, 0.f, 0.f, 0.f};
+                L = 0.f;
+                for (int w = 0; w < NWS; w++) {
+                    const float2 q = s_ml[wave + w][lane];
+                    const float4 v = s_acc[wave + w][lane];
+                    const float f = __builtin_amdgcn_exp2f(q.x - M);
+                    L += f * q.y;
+                    acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+                }
+            }
+        }
+        if (ws == 0 && live) {
+            const float inv = L == 0.f ? 0.f : 1.0f / L;   // padding left zeros and sums of zero
+            const int head = mg.kv_head * G + r % G, tok = mg.tok0 + r / G;
+            uint2 w;
+            w.x = pack_bf16(acc.x * inv, acc.y * inv);
+            w.y = pack_bf16(acc.z * inv, acc.w * inv);
+            *reinterpret_cast<uint2*>(a.out + (a.ldo ? (size_t)tok * a.ldo + head * D + col : act_offset(tok, head * D + col, a.n_q * D))) = w;
+        }
+        if (NWS > 1) __syncthreads();  // the next pass overwrites the LDS slots
+    }
+}
+
+int tree_tokens_per_item(int G, int nt) { return TREE_WAVES * nt * (16 / G); }
+
+template <int D, int G>
+static hipError_t launch_dg(const TreeArgs& a_in, hipStream_t st) {
+    TreeArgs a = a_in;
+    a.team_per_xcd = (a.n_team + 7) >> 3;
+    a.wave_blocks_per_xcd = ((a.n_workers - a.n_team + TREE_WAVES - 1) / TREE_WAVES + 7) >> 3;
+    const dim3 grid((a.team_per_xcd + a.wave_blocks_per_xcd) * 8), block(64 * TREE_WAVES);
+    if (a.ev_begin) (void)hipEventRecord(a.ev_begin, st);
+    switch (a.nt) {
+        case 3: hipLaunchKernelGGL((tree_kernel<D, G, 3>), grid, block, 0, st, a); break;
+        default: return hipErrorInvalidValue;
+    }
+    hipError_t e = hipGetLastError();
+    if (a.ev_end) (void)hipEventRecord(a.ev_end, st);
+    if (e != hipSuccess || a.n_groups == 0) return e;
+    // wavefronts of a block: for the most splits times the most passes (a power of two each) of any group
+    const int passes = (std::max(1, a.max_merge_rows) * (D / 4) + 63) / 64;
+    int nw = merge_split_waves(a.max_splits, MERGE_MAX_WAVES);
+    for (int p = 1; p < passes && nw < MERGE_MAX_WAVES; p *= 2) nw *= 2;
+    hipLaunchKernelGGL((tree_merge_kernel<D, G>), dim3(merge_blocks(a.n_groups)), dim3(64 * nw), 0, st, a);
+    return hipGetLastError();
+}
+
+template <int D>
+static hipError_t launch_d(const TreeArgs& a, hipStream_t st) {
+    switch (a.n_q / a.n_kv) {
+        case 1: return launch_dg<D, 1>(a, st);
+        case 2: return launch_dg<D, 2>(a, st);
+        case 4: return launch_dg<D, 4>(a, st);
+        case 8: return launch_dg<D, 8>(a, st);
+        case 16: return launch_dg<D, 16>(a, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t st) {
+    if (a.n_items <= 0 || a.n_workers <= 0) return hipSuccess;
+    if (a.n_team < 0 || a.n_team > a.n_workers) return hipErrorInvalidValue;
+    if (a.d == 128) return launch_d<128>(a, st);
+    if (a.d == 64) return launch_d<64>(a, st);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace ps

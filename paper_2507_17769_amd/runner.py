@@ -1,6 +1,8 @@
 """Convenience wrapper used by the tests, the smoke entry and the benchmark: owns a library
 context plus the torch tensors (device memory only) that feed it.  All computation happens in
 libpolystep; torch allocates buffers and moves bytes."""
+import ctypes as C
+
 import numpy as np
 import torch
 
@@ -15,6 +17,22 @@ def bits_to_dev(bits, device):
 
 def dev_to_bits(t):
     return t.detach().cpu().contiguous().view(torch.int16).numpy().view(np.uint16)
+
+
+class _PoolMemory:
+    """The KV pool as torch sees foreign device memory; keeps the context that owns it alive."""
+
+    def __init__(self, ctx):
+        self.ctx = ctx
+        address, n_bytes = ctx.kv_pool()
+        self.__cuda_array_interface__ = {"shape": (n_bytes // 2,), "typestr": "<i2", "data": (address, False), "version": 3}
+
+
+def _dtype_code(t):
+    codes = {torch.float32: B.PS_F32, torch.bfloat16: B.PS_BF16}
+    if t.dtype not in codes:
+        raise TypeError(f"expected a float32 or bfloat16 tensor, not {t.dtype}")
+    return codes[t.dtype]
 
 
 class Engine:
@@ -105,3 +123,131 @@ class Engine:
             out_dev = torch.empty_like(x_dev)
         stats = self.ctx.step(seqs, x_dev.data_ptr(), out_dev.data_ptr(), want_stats)
         return out_dev, stats
+
+    # ---- drafted tokens -------------------------------------------------------------------------------------------
+    def _rows(self, t, n_rows, width, name, dtypes=(torch.float32, torch.bfloat16)):
+        """Address and row stride of a device tensor whose leading dimension is rows of `width` adjacent elements."""
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the engine on {self.device}")
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name} has type {t.dtype}")
+        if t.dim() < 2 or t.shape[0] != n_rows or t[:1].numel() != (width if n_rows else 0):
+            raise ValueError(f"{name} must hold {n_rows} rows of {width}, not {tuple(t.shape)}")
+        if n_rows and not t[0].is_contiguous():
+            raise ValueError(f"the elements of a row of {name} must be adjacent")
+        return t.data_ptr(), (t.stride(0) if n_rows > 1 else max(width, t.stride(0)))
+
+    def kv_pool(self):
+        """The KV pool as a bf16 tensor [KV slot][page][kv head][K, V][16 * head_dim] (a view: see ps_kv_pool for the order of a
+        page's elements).  It keeps the context alive; ctx.kv_alloc or close() end it."""
+        m = self.model
+        flat = torch.as_tensor(_PoolMemory(self.ctx), device=self.device).view(torch.bfloat16)
+        return flat.view(-1, self.n_pool_pages, m["n_kv"], 2, 16 * m["head_dim"])
+
+    def tree(self, seqs, parents=None):
+        """A planned batch of token trees; .plan(seqs, parents) plans it anew."""
+        return B.Tree(self.ctx).plan(seqs, parents)
+
+    def load_qk_norm(self, layer, g_q, g_k):
+        """Gains [head_dim] (device bf16 tensors) of a layer that normalises its query and key heads; None, None: it does not."""
+        d = self.model["head_dim"]
+        if g_q is None and g_k is None:
+            self.ctx.init_qk_norm(layer, None, None)
+            return
+        gains = [g.to(device=self.device, dtype=torch.bfloat16).contiguous() for g in (g_q, g_k)]
+        if any(g.shape != (d,) for g in gains):
+            raise ValueError(f"gains must hold {d} elements")
+        self.ctx.init_qk_norm(layer, gains[0].data_ptr(), gains[1].data_ptr())
+        self.ctx.sync()
+
+    def qk_norm_rope(self, layer, tree, qkv, q=None):
+        """qkv: [T][(n_q + 2 n_kv) * head_dim] fp32 or bf16, any row stride.  Appends keys and values; returns bf16 [T][n_q][head_dim]."""
+        m = self.model
+        p, ld = self._rows(qkv, tree.n_tokens, (m["n_q"] + 2 * m["n_kv"]) * m["head_dim"], "qkv")
+        if q is None:
+            q = torch.empty((tree.n_tokens, m["n_q"], m["head_dim"]), dtype=torch.bfloat16, device=self.device)
+        elif q.shape != (tree.n_tokens, m["n_q"], m["head_dim"]) or q.dtype != torch.bfloat16 or not q.is_contiguous() or q.device != self.device:
+            raise ValueError("q must be a contiguous bf16 [T][n_q][head_dim] tensor of the engine's device")
+        self.ctx.qk_norm_rope(layer, tree, p, _dtype_code(qkv), ld, q.data_ptr())
+        return q
+
+    def tree_attention(self, layer, tree, q, out=None):
+        """q: bf16 [T][n_q][head_dim], any row stride; returns the same shape."""
+        m = self.model
+        width = m["n_q"] * m["head_dim"]
+        pq, ldq = self._rows(q, tree.n_tokens, width, "q", (torch.bfloat16,))
+        if out is None:
+            out = torch.empty((tree.n_tokens, m["n_q"], m["head_dim"]), dtype=torch.bfloat16, device=self.device)
+        po, ldo = self._rows(out, tree.n_tokens, width, "out", (torch.bfloat16,))
+        self.ctx.tree_attention(layer, tree, pq, ldq, po, ldo)
+        return out
+
+    def tree_keep(self, tree, kept):
+        """kept: for each sequence the nodes whose cache rows become the prefix's next positions, ascending."""
+        self.ctx.tree_keep(tree, kept)
+
+    def _rules(self, rules, n_rows):
+        """rules: dict of device tensors with the names of ps_logit_rules ("mask" int32 [n_masks][words])."""
+        r = B.ps_logit_rules()
+        floats = ("repetition", "frequency", "presence", "bias_value")
+        known = {n for n, t in B.ps_logit_rules._fields_ if t is C.c_void_p}
+        for name, t in rules.items():
+            if name not in known:
+                raise ValueError(f"unknown rule {name}")
+            if t is None:
+                continue
+            if t.device != self.device or t.dtype != (torch.float32 if name in floats else torch.int32):
+                raise TypeError(f"{name} must be a {'float32' if name in floats else 'int32'} tensor of the engine's device")
+            if name != "mask" and (t.dim() != 1 or not t.is_contiguous()):
+                raise ValueError(f"{name} must be one contiguous row")
+            if name == "mask" and (t.dim() != 2 or (t.numel() and t.stride(1) != 1)):
+                raise ValueError("mask must hold rows of adjacent words")
+            if t.numel():
+                setattr(r, name, t.data_ptr())
+        got = {k: t for k, t in rules.items() if t is not None}
+        lists = {k: got[k].shape[0] for k in ("repetition", "frequency", "presence", "output_begin") if k in got}
+        lists.update({k: got[k].shape[0] - 1 for k in ("history_begin", "bias_begin") if k in got})
+        if len(set(lists.values())) > 1:
+            raise ValueError(f"the rules disagree about the number of lists: {lists}")
+        r.n_lists = next(iter(lists.values()), 0)
+        r.n_history = got["history"].shape[0] if "history" in got else 0
+        r.n_biases = got["bias_token"].shape[0] if "bias_token" in got else 0
+        if r.n_history == 0:
+            r.history = r.output_begin = None
+        if "bias_token" in got and ("bias_value" not in got or got["bias_value"].shape != got["bias_token"].shape):
+            raise ValueError("bias_value must hold one value per bias_token")
+        for name in ("mask_row", "row_list", "row_token", "row_prev"):
+            if name in got and got[name].shape[0] != n_rows:
+                raise ValueError(f"{name} must hold one entry per row")
+        if r.mask:
+            r.n_masks, r.mask_stride = got["mask"].shape[0], max(got["mask"].shape[1], got["mask"].stride(0))
+        else:
+            r.mask_row = None
+        return r
+
+    def pick_tokens(self, logits, rules=None, want_logits=False):
+        """logits: [rows][vocab] fp32 or bf16, any row stride.  Returns {"next": int32 [rows], "logprob": fp32 [rows]} and, if wanted,
+        "logits": the changed ones, fp32 [rows][vocab]."""
+        if logits.dim() != 2:
+            raise ValueError("logits must be [rows][vocab]")
+        n, vocab = logits.shape
+        p, ld = self._rows(logits, n, vocab, "logits")
+        out = {"next": torch.empty(n, dtype=torch.int32, device=self.device), "logprob": torch.empty(n, dtype=torch.float32, device=self.device)}
+        if want_logits:
+            out["logits"] = torch.empty((n, vocab), dtype=torch.float32, device=self.device)
+        self.ctx.pick_tokens(p, _dtype_code(logits), ld, n, vocab, None if rules is None else self._rules(rules, n),
+                             out["logits"].data_ptr() if want_logits else None, vocab, out["next"].data_ptr(), out["logprob"].data_ptr())
+        return out
+
+    def verify_tokens(self, tree, token_ids, rules=None, want_logits=False, want_hidden=False):
+        """Full-model step over a batch of trees: token_ids host [T].  Returns {"next", "logprob"} for every node, optionally "logits"
+        (changed by the rules) and "hidden"."""
+        T = tree.n_tokens
+        out = {"next": torch.empty(T, dtype=torch.int32, device=self.device), "logprob": torch.empty(T, dtype=torch.float32, device=self.device)}
+        if want_logits:
+            out["logits"] = torch.empty((T, self.vocab), dtype=torch.float32, device=self.device)
+        if want_hidden:
+            out["hidden"] = torch.empty((T, self.model["hidden"]), dtype=torch.float32, device=self.device)
+        self.ctx.verify_tokens(tree, token_ids, None if rules is None else self._rules(rules, T), out["next"].data_ptr(), out["logprob"].data_ptr(),
+                               out["logits"].data_ptr() if want_logits else None, out["hidden"].data_ptr() if want_hidden else None)
+        return out
