@@ -178,11 +178,11 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
 // The same for batches whose new tokens form trees (tree_attention.hip).
 struct TreeArgs : AttnArgs {
     const uint32_t* masks;   // see AttnItem
-    int nt;                  // 16-row tiles of a team's wavefront
     int64_t ldo;             // row stride of out in elements; 0: operand order
+    bool pages_once;         // no sequence has more than one query block
 };
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t st);
-int tree_tokens_per_item(int G, int nt);   // of a team with nt tiles to a wavefront
+int tree_tokens_per_item(int G);   // of a team, at most
 
 // Normalise the heads of queries and keys, rotate, append (qk_norm.hip).
 struct NormRopeArgs {

@@ -90,9 +90,9 @@ ps_status send(ps_ctx* c, ps_tree::Pinned& b, void* dev, size_t bytes) {
     return PS_OK;
 }
 
-PlanConfig tree_plan_config(const ps_ctx* c, int nt) {
+PlanConfig tree_plan_config(const ps_ctx* c) {
     PlanConfig pc = plan_config(c);
-    pc.prefill_tokens = tree_tokens_per_item(pc.group, nt);
+    pc.prefill_tokens = tree_tokens_per_item(pc.group);
     return pc;
 }
 
@@ -225,13 +225,12 @@ extern "C" ps_status ps_tree_plan(ps_ctx* c, ps_tree* t, const ps_seq* seqs, int
         if (!c->host_only && !c->pool) return fail(c, PS_ESTATE, "ps_tree_plan: no KV pool (call ps_kv_alloc)");
         OnDevice on(c);
         std::string err;
-        const int nt = 3;
-        const PlanConfig pc = tree_plan_config(c, nt);
+        const PlanConfig pc = tree_plan_config(c);
         ps_status st = validate_batch(seqs, n_seqs, pc, c->page_seen, err);
         if (st == PS_OK) st = build_tree_plan(seqs, n_seqs, parents, pc, t->plan, err);
         if (st != PS_OK) return fail(c, st, "ps_tree_plan: " + err);
         t->args = TreeArgs{};
-        t->args.nt = nt;
+        t->args.pages_once = std::all_of(t->plan.seqs.begin(), t->plan.seqs.end(), [&](const SeqInfo& s) { return s.n_new <= pc.prefill_tokens; });
         if (!c->host_only && n_seqs > 0 && (st = upload(c, t, t->plan)) != PS_OK) return st;
         t->pool_id = c->pool_id;
         t->planned = true;

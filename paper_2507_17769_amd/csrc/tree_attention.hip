@@ -11,16 +11,30 @@
 //
 // A masked place may hold anything, infinities and NaN too (a rejected branch of an overflowed draft; a page's tail that nobody
 // wrote): its score is replaced, and its value must not reach a row that does not see it, which a zero weight alone does not
-// give (0 * inf is NaN).  In the masked pairs non-finite values are taken out of the product, and where there are any, what
-// the rows that do see them get is counted with three more products (see pv_masked).
+// give (0 * inf is NaN).  In the masked pairs non-finite values are taken out of the product; where there were any, the rows that
+// do see them get them at the end of the item (see add_specials).
 #include "attention_device.h"
 
 #include <algorithm>
 
 namespace ps {
 
-constexpr int TREE_WAVES = 4;
-constexpr int TREE_RING = 3;   // pairs of pages in LDS: the one in use, and two on their way
+constexpr int TREE_WAVES = 4;   // of a block, of which a compute unit holds two
+constexpr int TREE_NT = 3;      // query tiles of a wavefront, at most
+constexpr int TREE_RING = 4;    // pairs of pages in LDS
+
+// As PS_GLOBAL_TO_LDS, with the non-temporal hint: for pages that are read once.
+__device__ __forceinline__ void global_to_lds_stream(const uint8_t* src, uint8_t* dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 2);
+}
+
+// The lane, formed anew for every item: what follows from it would otherwise be hoisted out of the loop over the items, for all kinds of
+// item at once, and hold 28 registers through the loops over the pairs.
+__device__ __forceinline__ int lane_id() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t & 63;
+}
 
 // What the row of token `qc` of the item's block sees of the 32 positions 32 pair .. 32 pair + 31.
 __device__ __forceinline__ uint32_t visible_word(const TreeArgs& a, const AttnItem& it, int qc, int pair) {
@@ -50,55 +64,91 @@ __device__ __forceinline__ u32x4_t class_of(u32x4_t v, int cls) {
     for (int i = 0; i < 4; i++) o[i] = half_class(v[i] & 0xFFFFu, cls) | (half_class(v[i] >> 16, cls) << 16);
     return o;
 }
-__device__ __forceinline__ u32x4_t without_specials(u32x4_t v) {
-    u32x4_t o;
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        o[i] = ((v[i] & 0x7F80u) == 0x7F80u ? 0u : v[i] & 0xFFFFu) | ((v[i] & 0x7F800000u) == 0x7F800000u ? 0u : v[i] & 0xFFFF0000u);
-    return o;
+__device__ __forceinline__ uint32_t without_specials(uint32_t w) {
+    return ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u);
 }
-__device__ __forceinline__ bool has_specials(u32x4_t v) {
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < 4; i++) any = any || (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
-    return any;
+// of two packed pairs, the larger magnitude of either place; a pair with a magnitude of infinity or above
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t larger_halves(uint32_t x, uint32_t y) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, x & 0x7FFF7FFFu), __builtin_bit_cast(u16x2_t, y & 0x7FFF7FFFu)));
 }
+__device__ __forceinline__ bool is_special(uint32_t w) { return (w & 0x7FFFu) >= 0x7F80u || (w & 0x7FFF0000u) >= 0x7F800000u; }
+__device__ __forceinline__ bool has_specials(u32x4_t v) { return is_special(larger_halves(larger_halves(v[0], v[1]), larger_halves(v[2], v[3]))); }
 __device__ __forceinline__ f32x4_t mfma_16x16x32(u32x4_t a, bf16x8_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), b, c, 0, 0, 0);
 }
 
-// o += V^T P^T for one d-tile (16 values of d) of a masked pair.  v: the lane's eight values (d = lane % 16; tokens 4 g .. of either page),
-// seen: ones where the lane's row sees the token.
-__device__ __forceinline__ f32x4_t pv_masked(f32x4_t o, u32x4_t v, bf16x8_t p, bf16x8_t seen) {
-    o = mfma_16x16x32(without_specials(v), p, o);
-    if (__builtin_amdgcn_ballot_w64(has_specials(v)) == 0) return o;
-    const f32x4_t none = {0.f, 0.f, 0.f, 0.f};
-    const f32x4_t up = mfma_16x16x32(class_of(v, POS_INF), seen, none), down = mfma_16x16x32(class_of(v, NEG_INF), seen, none),
-                  nan = mfma_16x16x32(class_of(v, NOT_A_NUMBER), seen, none);
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        if (up[i] > 0.f) o[i] += __builtin_inff();
-        if (down[i] > 0.f) o[i] -= __builtin_inff();
-        if (nan[i] > 0.f) o[i] = __builtin_nanf("");
-    }
-    return o;
+__device__ __forceinline__ bf16_t* out_at(const TreeArgs& a, size_t tok, int col) {
+    return a.out + (a.ldo ? tok * a.ldo + col : act_offset((int)tok, col, a.n_q * a.d));
 }
 
-// Scores of the keys that a row does not see become -inf: the running maximum starts at a large finite negative number, so a
-// row that has seen nothing keeps it and gets weights of zero.  word: see visible_word; g: the lane's key group.
-__device__ __forceinline__ bf16x8_t hide(f32x4_t& sa, f32x4_t& sb, uint32_t word, int g) {
+// Ones where the lane's row sees the token: bits of a word (see visible_word) as an operand; g: the lane's key group.
+__device__ __forceinline__ bf16x8_t seen_operand(uint32_t word, int g) {
     const uint32_t w = word >> (4 * g);
     u32x4_t seen;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        sa[i] = (w >> i) & 1u ? sa[i] : -__builtin_inff();
-        sb[i] = (w >> (16 + i)) & 1u ? sb[i] : -__builtin_inff();
-    }
     seen[0] = (w & 1u ? 0x3F80u : 0u) | (w & 2u ? 0x3F800000u : 0u);
     seen[1] = (w & 4u ? 0x3F80u : 0u) | (w & 8u ? 0x3F800000u : 0u);
     seen[2] = (w & 0x10000u ? 0x3F80u : 0u) | (w & 0x20000u ? 0x3F800000u : 0u);
     seen[3] = (w & 0x40000u ? 0x3F80u : 0u) | (w & 0x80000u ? 0x3F800000u : 0u);
     return __builtin_bit_cast(bf16x8_t, seen);
+}
+
+// After an item's rows have been stored: the non-finite values of its masked pairs, which the products left out, go to the rows that see
+// them.  Three products of ones count, for each row and value of d, the +inf, -inf and NaN that it sees; every lane mends what it
+// stored itself.  Rare, so it may read everything once more.
+template <int D, int G, int NT>
+__device__ __forceinline__ void add_specials(const TreeArgs& a, const AttnItem& it, int tok_row, int slot0, int first_pair, int last_pair, int lane) {
+    constexpr int DT = D / 16, TQ = 16 / G;
+    const int r = lane & 15, g = lane >> 4;
+    const int32_t* pages = a.pages + it.page_off;
+    const size_t page_stride = (size_t)a.n_kv * 2 * 16 * D;
+    const bf16_t* v_lane = a.pool_slot + (size_t)it.kv_head * 2 * 16 * D + 16 * D + (size_t)lane * 8;
+#pragma unroll 1
+    for (int j = first_pair * DT; j < (last_pair + 1) * DT; j++) {
+        const int pair = j / DT, dt = j % DT;
+        const size_t at = (dt >> 1) * 512 + 4 * (dt & 1);
+        const uint2 x = *reinterpret_cast<const uint2*>(v_lane + (size_t)pages[2 * pair] * page_stride + at);
+        const uint2 y = *reinterpret_cast<const uint2*>(v_lane + (size_t)pages[min(2 * pair + 1, it.page_end - 1)] * page_stride + at);
+        const u32x4_t v = {x.x, x.y, y.x, y.y};
+        if (__builtin_amdgcn_ballot_w64(has_specials(v)) == 0) continue;
+#pragma unroll 1
+        for (int nt = 0; nt < NT; nt++) {
+            const int qc = tok_row + nt * TQ;
+            const bf16x8_t seen = seen_operand(visible_word(a, it, min(qc, it.q_ntok - 1), pair), g);
+            const f32x4_t none = {0.f, 0.f, 0.f, 0.f};
+            const f32x4_t up = mfma_16x16x32(class_of(v, POS_INF), seen, none), down = mfma_16x16x32(class_of(v, NEG_INF), seen, none),
+                          nan = mfma_16x16x32(class_of(v, NOT_A_NUMBER), seen, none);
+            if (qc >= it.q_ntok || is_padding(a, it, qc)) continue;
+            float add[4];
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                add[i] = nan[i] > 0.f || (up[i] > 0.f && down[i] > 0.f) ? __builtin_nanf("") : up[i] > 0.f ? __builtin_inff() : down[i] > 0.f ? -__builtin_inff() : 0.f;
+                any = any || add[i] != 0.f;
+            }
+            if (!any) continue;
+            if (it.partial < 0) {
+                uint2* p = reinterpret_cast<uint2*>(out_at(a, (size_t)it.tok_g0 + qc, (it.kv_head * G + r % G) * D + 16 * dt + 4 * g));
+                const uint2 w = *p;
+                *p = uint2{pack_bf16(bf16_lo(w.x) + add[0], bf16_hi(w.x) + add[1]), pack_bf16(bf16_lo(w.y) + add[2], bf16_hi(w.y) + add[3])};
+            } else {
+                float4* p = reinterpret_cast<float4*>(a.part_o + (((size_t)it.partial + slot0 + nt) * 16 + r) * D + 16 * dt + 4 * g);
+                const float4 w = *p;
+                *p = float4{w.x + add[0], w.y + add[1], w.z + add[2], w.w + add[3]};
+            }
+        }
+    }
+}
+
+// Scores of the keys that a row does not see become -inf: the running maximum starts at a large finite negative number, so a
+// row that has seen nothing keeps it and gets weights of zero.
+__device__ __forceinline__ void hide(f32x4_t& sa, f32x4_t& sb, uint32_t word, int g) {
+    const uint32_t w = word >> (4 * g);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        sa[i] = (w >> i) & 1u ? sa[i] : -__builtin_inff();
+        sb[i] = (w >> (16 + i)) & 1u ? sb[i] : -__builtin_inff();
+    }
 }
 
 // Softmax of one tile for a pair: raw scores -> P as a packed operand, running maximum m (in the scores' units) and the factor
@@ -149,7 +199,11 @@ __device__ __forceinline__ void rescale(f32x4_t (&o)[DT], f32x4_t& l, float alph
 
 // End of an item: the NT tiles of a wavefront go to the output (normalised) or, for an item that covers only part of its KV span, to
 // partial slots it.partial + slot0 + nt.  l: each row's sum, the same in the four lanes that share the row.  Padding gets zeros.
-template <int D, int G, int NT>
+// Which 16 values of d accumulator dt holds: swapped accumulators (see team_pair) hold the neighbour's in the lanes of g >= 2.
+template <bool SWAP>
+__device__ __forceinline__ int dt_of(int dt, int g) { return SWAP ? dt ^ (g >> 1) : dt; }
+
+template <int D, int G, int NT, bool SWAP>
 __device__ __forceinline__ void store_rows(const TreeArgs& a, const AttnItem& it, const f32x4_t (&o)[NT][D / 16], const float (&m)[NT], const float (&l)[NT],
                                            int tok_row, int slot0, int lane) {
     constexpr int DT = D / 16, TQ = 16 / G;
@@ -165,18 +219,18 @@ __device__ __forceinline__ void store_rows(const TreeArgs& a, const AttnItem& it
             const size_t tok = (size_t)it.tok_g0 + qc;
 #pragma unroll
             for (int dt = 0; dt < DT; dt++) {
-                const int col = head * D + 16 * dt + 4 * g;
+                const int col = head * D + 16 * dt_of<SWAP>(dt, g) + 4 * g;
                 uint2 w;
                 w.x = padding ? 0u : pack_bf16(o[nt][dt][0] * inv, o[nt][dt][1] * inv);
                 w.y = padding ? 0u : pack_bf16(o[nt][dt][2] * inv, o[nt][dt][3] * inv);
-                *reinterpret_cast<uint2*>(a.out + (a.ldo ? tok * a.ldo + col : act_offset((int)tok, col, a.n_q * D))) = w;
+                *reinterpret_cast<uint2*>(out_at(a, tok, col)) = w;
             }
         } else {
             const size_t slot = (size_t)it.partial + slot0 + nt;
             float* po = a.part_o + (slot * 16 + r) * D + 4 * g;
 #pragma unroll
             for (int dt = 0; dt < DT; dt++)
-                *reinterpret_cast<float4*>(po + 16 * dt) =
+                *reinterpret_cast<float4*>(po + 16 * dt_of<SWAP>(dt, g)) =
                     padding ? float4{0.f, 0.f, 0.f, 0.f} : float4{o[nt][dt][0], o[nt][dt][1], o[nt][dt][2], o[nt][dt][3]};
             if (g == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * 16 + r) * 2) = padding ? float2{NEG_BIG, 0.f} : float2{m[nt], l[nt]};
         }
@@ -186,7 +240,7 @@ __device__ __forceinline__ void store_rows(const TreeArgs& a, const AttnItem& it
 // ---- single-tile blocks: one wavefront -------------------------------------------------------------
 // The next pair of pages is in flight in a second register set while the current one is consumed.
 template <int D, bool MASK>
-__device__ __forceinline__ void wave_pair(f32x4_t (&o)[1][D / 16], f32x4_t& lacc, float& m, const PairRegs<D / 32>& p, const bf16x8_t (&qf)[D / 32],
+__device__ __forceinline__ void wave_pair(f32x4_t (&o)[1][D / 16], f32x4_t& lacc, float& m, bool& specials, PairRegs<D / 32>& p, const bf16x8_t (&qf)[D / 32],
                                           uint32_t word, int g, float scale2) {
     constexpr int KS = D / 32, DT = D / 16;
     f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
@@ -196,25 +250,45 @@ __device__ __forceinline__ void wave_pair(f32x4_t (&o)[1][D / 16], f32x4_t& lacc
         sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(p.kb[s]), qf[s], sb, 0, 0, 0);
     }
     matrix_results(sa, sb);
-    bf16x8_t seen;
-    if constexpr (MASK) seen = hide(sa, sb, word, g);
+    if constexpr (MASK) {
+        hide(sa, sb, word, g);
+        uint32_t largest = 0;
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+            largest = larger_halves(largest, larger_halves(larger_halves(p.va[s].x, p.va[s].y), larger_halves(p.va[s].z, p.va[s].w)));
+            largest = larger_halves(largest, larger_halves(larger_halves(p.vb[s].x, p.vb[s].y), larger_halves(p.vb[s].z, p.vb[s].w)));
+        }
+        if (__builtin_amdgcn_ballot_w64(is_special(largest)) != 0) {
+            specials = true;
+#pragma unroll
+            for (int s = 0; s < KS; s++) {
+                p.va[s] = uint4{without_specials(p.va[s].x), without_specials(p.va[s].y), without_specials(p.va[s].z), without_specials(p.va[s].w)};
+                p.vb[s] = uint4{without_specials(p.vb[s].x), without_specials(p.vb[s].y), without_specials(p.vb[s].z), without_specials(p.vb[s].w)};
+            }
+        }
+    }
     float alpha;
     const bf16x8_t pf = tile_softmax(sa, sb, m, alpha, scale2);
     rescale<DT>(o[0], lacc, alpha);
     lacc = mfma_16x16x32(ONES, pf, lacc);
+    // one product per page and d-tile: each 8-byte half of a loaded register quad is an operand as it stands, where one for both pages would
+    // take 64 register moves
+    const uint4 pw = __builtin_bit_cast(uint4, pf);
+    const s16x4_t pa = __builtin_bit_cast(s16x4_t, uint2{pw.x, pw.y}), pb = __builtin_bit_cast(s16x4_t, uint2{pw.z, pw.w});
 #pragma unroll
     for (int dt = 0; dt < DT; dt++) {
         const int s = dt >> 1;
-        const u32x4_t v = (dt & 1) ? u32x4_t{p.va[s].z, p.va[s].w, p.vb[s].z, p.vb[s].w} : u32x4_t{p.va[s].x, p.va[s].y, p.vb[s].x, p.vb[s].y};
-        if constexpr (MASK) o[0][dt] = pv_masked(o[0][dt], v, pf, seen);
-        else o[0][dt] = mfma_16x16x32(v, pf, o[0][dt]);
+        const uint2 wa = (dt & 1) ? uint2{p.va[s].z, p.va[s].w} : uint2{p.va[s].x, p.va[s].y};
+        const uint2 wb = (dt & 1) ? uint2{p.vb[s].z, p.vb[s].w} : uint2{p.vb[s].x, p.vb[s].y};
+        o[0][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, wa), pa, o[0][dt], 0, 0, 0);
+        o[0][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, wb), pb, o[0][dt], 0, 0, 0);
     }
 }
 
 template <int D, int G>
 __device__ __forceinline__ void wave_item(const TreeArgs& a, const AttnItem it) {
     constexpr int KS = D / 32, DT = D / 16;
-    const int lane = threadIdx.x & 63;
+    const int lane = lane_id();
     const int r = lane & 15, g = lane >> 4;
     const int32_t* pages = a.pages + it.page_off;
     const int head = it.kv_head * G + (r % G);
@@ -225,54 +299,67 @@ __device__ __forceinline__ void wave_item(const TreeArgs& a, const AttnItem it) 
     for (int s = 0; s < KS; s++) qf[s] = as_bf16x8(ldg16(qrow + 32 * s));
     f32x4_t o[1][DT], lacc = {0.f, 0.f, 0.f, 0.f};
     float m = NEG_BIG;
+    bool specials = false;
 #pragma unroll
     for (int dt = 0; dt < DT; dt++) o[0][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);  // log2(e)/sqrt(d): softmax in base 2
     const size_t page_stride = (size_t)a.n_kv * 2 * 16 * D;
     const bf16_t* pool_lane = a.pool_slot + (size_t)it.kv_head * 2 * 16 * D + (size_t)lane * 8;
-
-    const int n_pg = it.page_end - it.page_begin, n_pairs = (n_pg + 1) >> 1, pair0 = it.page_begin >> 1;
-    const int n_free = max(0, min(n_pairs, first_masked_pair(it, it.pos0) - pair0));   // pairs without a mask
-    // page ids 64 at a time, lane l holding page tb0 + l of the item's range
-    int tb0 = 0, tbl = pages[it.page_begin + min(lane, n_pg - 1)];
-    auto load = [&](PairRegs<KS>& p, int i) {   // i < n_pairs
-        if (2 * i >= tb0 + 64) {
-            tb0 += 64;
-            tbl = pages[it.page_begin + tb0 + min(lane, n_pg - tb0 - 1)];
+    const int masked = first_masked_pair(it, it.pos0);
+    // Pages in blocks of up to 64: lane l keeps the id of the block's page l, and a uniform readlane hands the ids out, so no load
+    // sits between a pair's id and its data.  The item carries its first two ids: the first loads do not wait for the others.
+    for (int blk = it.page_begin; blk < it.page_end; blk += 64) {
+        const int n_pg = min(64, it.page_end - blk);
+        const int my_pid = pages[blk + min(lane, n_pg - 1)];
+        const int n_pairs = (n_pg + 1) >> 1, pair0 = blk >> 1;
+        auto load = [&](PairRegs<KS>& p, int i) {
+            load_pair<D>(p, pool_lane, page_stride, __builtin_amdgcn_readlane(my_pid, 2 * i), __builtin_amdgcn_readlane(my_pid, min(2 * i + 1, n_pg - 1)));
+        };
+        // two register sets; the steady body issues its loads unconditionally, so that the wait before each computation covers
+        // exactly the older set
+        PairRegs<KS> b0, b1;
+        if (blk == it.page_begin) load_pair<D>(b0, pool_lane, page_stride, it.page0, it.page1);
+        else load(b0, 0);
+        const int n_free = min(n_pairs, masked - pair0);
+        int i = 0;
+        for (; i + 2 < n_free; i += 2) {
+            load(b1, i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            wave_pair<D, false>(o, lacc, m, specials, b0, qf, 0, g, scale2);
+            __builtin_amdgcn_sched_barrier(0);
+            load(b0, i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            wave_pair<D, false>(o, lacc, m, specials, b1, qf, 0, g, scale2);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        const int la = 2 * i - tb0;
-        load_pair<D>(p, pool_lane, page_stride, __builtin_amdgcn_readlane(tbl, la), __builtin_amdgcn_readlane(tbl, min(la + 1, n_pg - tb0 - 1)));
-    };
-    PairRegs<KS> b0, b1;
-    load(b0, 0);
-    int i = 0;
-    for (; i + 2 <= n_free; i += 2) {
-        load(b1, i + 1);
-        __builtin_amdgcn_sched_barrier(0);
-        wave_pair<D, false>(o, lacc, m, b0, qf, 0, g, scale2);
-        __builtin_amdgcn_sched_barrier(0);
-        load(b0, min(i + 2, n_pairs - 1));   // past the last pair: that pair again, not used
-        __builtin_amdgcn_sched_barrier(0);
-        wave_pair<D, false>(o, lacc, m, b1, qf, 0, g, scale2);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    // an odd pair of the prefix and the masked pairs, one at a time
-    for (; i < n_pairs; i++) {
-        load(b1, min(i + 1, n_pairs - 1));
-        wave_pair<D, true>(o, lacc, m, b0, qf, i < n_free ? 0xFFFFFFFFu : visible_word(a, it, qc, pair0 + i), g, scale2);
-        b0 = b1;
+        // the last one or two pairs of the prefix in the block, and the masked ones, which the stream ends with
+        for (; i < n_pairs; i++) {
+            load(b1, min(i + 1, n_pairs - 1));
+            wave_pair<D, true>(o, lacc, m, specials, b0, qf, pair0 + i < masked ? 0xFFFFFFFFu : visible_word(a, it, qc, pair0 + i), g, scale2);
+#pragma unroll
+            for (int s = 0; s < KS; s++) { b0.ka[s] = b1.ka[s]; b0.kb[s] = b1.kb[s]; b0.va[s] = b1.va[s]; b0.vb[s] = b1.vb[s]; }
+        }
     }
     const float ml[1] = {rounded_product(m, scale2)}, l[1] = {lacc[0]};
-    store_rows<D, G, 1>(a, it, o, ml, l, r / G, 0, lane);
+    store_rows<D, G, 1, false>(a, it, o, ml, l, r / G, 0, lane);
+    if (specials) add_specials<D, G, 1>(a, it, r / G, 0, max(masked, it.page_begin >> 1), (it.page_end - 1) >> 1, lane);
 }
 
 // ---- teams: blocks of several tiles ---------------------------------------------------------------
 // One pair of pages from ring slot `addr` (LDS byte address of this lane's 16 bytes of the slot's first KiB) for the
-// wavefront's NT tiles.  The slot holds the pair as 4 KS KiB blocks [k-step s][K page a, K page b, V page a, V page b].
-template <int D, int NT, bool MASK>
-__device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&lacc)[NT], float (&m)[NT], uint32_t addr, const bf16x8_t (&qf)[NT][D / 32],
-                                          const uint32_t (&word)[NT], int g, float scale2) {
+// wavefront's NT tiles.  The slot holds the pair as 4 KS KiB blocks [k-step s][K page a, K page b, V page a, V page b].  A V operand is an 8-byte
+// half of a lane's 16 bytes: were it the same half in all lanes, two lanes would share each bank.  Lanes 8 .. 15 of every 16 read the other
+// one (vswap = 8), so accumulator dt holds in its rows 8 .. 15 the values of tile dt ^ 1: its lanes of g >= 2 (see dt_of).
+template <int D, int G, int NT, bool MASK>
+__device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&lacc)[NT], float (&m)[NT], bool& specials, uint32_t addr, const bf16x8_t (&qf)[NT][D / 32],
+                                          const TreeArgs& a, const AttnItem& it, int tok_row, int pair, int g, uint32_t vswap, float scale2) {
     constexpr int KS = D / 32, DT = D / 16;
+    uint32_t word[NT];
+    if constexpr (MASK) {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) word[nt] = visible_word(a, it, min(tok_row + nt * (16 / G), it.q_ntok - 1), pair);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     u32x4_t kk[2 * KS];
 #pragma unroll
     for (int s = 0; s < KS; s++) {
@@ -283,12 +370,6 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kk[0]), "+v"(kk[1]), "+v"(kk[2]), "+v"(kk[3]), "+v"(kk[4]), "+v"(kk[5]), "+v"(kk[6]), "+v"(kk[7]));
     else
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kk[0]), "+v"(kk[1]), "+v"(kk[2]), "+v"(kk[3]));
-    u32x2_t va[DT], vb[DT];
-#pragma unroll
-    for (int dt = 0; dt < DT; dt++) {
-        va[dt] = lds_read8(addr, (4 * (dt >> 1) + 2) * 1024 + 8 * (dt & 1));
-        vb[dt] = lds_read8(addr, (4 * (dt >> 1) + 3) * 1024 + 8 * (dt & 1));
-    }
     f32x4_t sa[NT], sb[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
@@ -300,21 +381,46 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
             sb[nt] = mfma_16x16x32(kk[2 * s + 1], qf[nt][s], sb[nt]);
         }
     }
+    __builtin_amdgcn_sched_barrier(0);   // the values after the keys: they take the keys' registers, and the softmax covers their way
+    u32x2_t va[DT], vb[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) {
+        const uint32_t half = (dt & 1) ? addr ^ vswap ^ 8 : addr ^ vswap;
+        va[dt] = lds_read8(half, (4 * (dt >> 1) + 2) * 1024);
+        vb[dt] = lds_read8(half, (4 * (dt >> 1) + 3) * 1024);
+    }
     if constexpr (NT == 1) matrix_results(sa[0], sb[0]);
     else if constexpr (NT == 2) matrix_results(sa[0], sb[0], sa[1], sb[1]);
     else matrix_results(sa[0], sb[0], sa[1], sb[1], sa[2], sb[2]);
-    bf16x8_t pf[NT], seen[NT];
+    bf16x8_t pf[NT];
     float alpha[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-        if constexpr (MASK) seen[nt] = hide(sa[nt], sb[nt], word[nt], g);
+        if constexpr (MASK) {
+            hide(sa[nt], sb[nt], word[nt], g);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         pf[nt] = tile_softmax(sa[nt], sb[nt], m[nt], alpha[nt], scale2);
+        if constexpr (MASK) __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (DT == 8)
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(va[1]), "+v"(va[2]), "+v"(va[3]), "+v"(va[4]), "+v"(va[5]), "+v"(va[6]), "+v"(va[7]),
                      "+v"(vb[0]), "+v"(vb[1]), "+v"(vb[2]), "+v"(vb[3]), "+v"(vb[4]), "+v"(vb[5]), "+v"(vb[6]), "+v"(vb[7]));
     else
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(va[1]), "+v"(va[2]), "+v"(va[3]), "+v"(vb[0]), "+v"(vb[1]), "+v"(vb[2]), "+v"(vb[3]));
+    if constexpr (MASK) {
+        uint32_t largest = 0;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) largest = larger_halves(largest, larger_halves(larger_halves(va[dt].x, va[dt].y), larger_halves(vb[dt].x, vb[dt].y)));
+        if (__builtin_amdgcn_ballot_w64(is_special(largest)) != 0) {
+            specials = true;
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) {
+                va[dt] = u32x2_t{without_specials(va[dt].x), without_specials(va[dt].y)};
+                vb[dt] = u32x2_t{without_specials(vb[dt].x), without_specials(vb[dt].y)};
+            }
+        }
+    }
     __builtin_amdgcn_s_setprio(1);   // the matrix unit is fed first (see attn_kernel)
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
@@ -323,42 +429,47 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
 #pragma unroll
         for (int dt = 0; dt < DT; dt++) {
             const u32x4_t v = {va[dt].x, va[dt].y, vb[dt].x, vb[dt].y};
-            if constexpr (MASK) o[nt][dt] = pv_masked(o[nt][dt], v, pf[nt], seen[nt]);
-            else o[nt][dt] = mfma_16x16x32(v, pf[nt], o[nt][dt]);
+            o[nt][dt] = mfma_16x16x32(v, pf[nt], o[nt][dt]);
         }
     }
     __builtin_amdgcn_s_setprio(0);
 }
 
-// One work item on a team.  Wavefront w holds the tiles NT w .. NT w + NT - 1 of the query block and copies the KS KiB blocks
-// w KS .. w KS + KS - 1 of every pair.  Pair i of the item's page range sits in ring slot i % 3.  Per pair: wait for the own copies of
-// this pair (those of the next may still be in flight), barrier (every wavefront's part has landed, and every wavefront has finished
-// with the pair before, whose slot is the one to refill), issue the copies of pair i + 2, compute.  Past the item's last pair the
-// copies fetch that last pair again, into slots nobody reads, so that the wait counts are the same in every trip.
-template <int D, int G, int NT>
+// One work item on a team.  The four wavefronts of the block are RW = 4 / KW row groups of NT tiles times KW key groups: with few tiles
+// the pairs of pages are dealt out to key groups, so that no wavefront is idle, and the groups' results are joined in LDS at the end.
+// Per round of KW pairs: wait for the own copies of this round (those of later rounds may still be in flight), barrier (every
+// wavefront's part has landed, and every wavefront has finished with the round before, whose slots are the ones to refill), issue
+// the copies of the round that takes those slots, compute.  Past the item's last pair the copies fetch that pair again, into slots nobody
+// reads, so that the wait counts are the same in every trip.
+template <int D, int G, int NT, int KW, bool ONCE>
 __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, uint8_t* ring, int wave) {
+    static_assert(KW == 1 || NT == 1, "the join holds one tile a wavefront");
     constexpr int KS = D / 32, DT = D / 16, TQ = 16 / G;
-    constexpr int PAIR_BYTES = 4 * KS * 1024;
-    const int lane = threadIdx.x & 63;
-    const int r = lane & 15, g = lane >> 4;
+    constexpr int RW = TREE_WAVES / KW, ROUNDS = TREE_RING / KW;   // rounds in the ring
+    constexpr int PAIR_BYTES = 4 * KS * 1024, LPW = 4 * KS / TREE_WAVES;   // KiB blocks of a pair that a wavefront copies
+    const int lane = lane_id();
+    const int r = lane & 15, g = lane >> 4, rg = wave % RW, kg = wave / RW;
     const int32_t* pages = a.pages + it.page_off;
     const int head = it.kv_head * G + (r % G);
 
-    // Row (lane r) of tile nt is token (wave NT + nt) TQ + r / G of the block, clamped to the block's last token (rows past it
+    // Row (lane r) of tile nt is token (rg NT + nt) TQ + r / G of the block, clamped to the block's last token (rows past it
     // compute on that token's data and are not stored).
-    const int tok_row = wave * NT * TQ + r / G;
+    const int tok_row = rg * NT * TQ + r / G;
     bf16x8_t qf[NT][KS];
+    auto load_queries = [&](int tok) {
 #pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-        const int qc = min(tok_row + nt * TQ, it.q_ntok - 1);
-        const bf16_t* qrow = a.q + (size_t)(it.tok_g0 + qc) * a.ldq + head * D + 8 * g;
+        for (int nt = 0; nt < NT; nt++) {
+            const int qc = min(tok + nt * TQ, it.q_ntok - 1);
+            const bf16_t* qrow = a.q + (size_t)(it.tok_g0 + qc) * a.ldq + head * D + 8 * g;
 #pragma unroll
-        for (int s = 0; s < KS; s++) qf[nt][s] = as_bf16x8(ldg16(qrow + 32 * s));
-    }
-    const int wave_tok0 = wave * NT * TQ;
-    const bool wave_has_rows = wave_tok0 < it.q_ntok;
-    const int pos_first = it.pos0 + min(wave_tok0, it.q_ntok - 1);
-    const int pos_last = it.pos0 + min(wave_tok0 + NT * TQ, it.q_ntok) - 1;   // nothing beyond is seen by any row of the wavefront
+            for (int s = 0; s < KS; s++) qf[nt][s] = as_bf16x8(ldg16(qrow + 32 * s));
+        }
+    };
+    load_queries(tok_row);
+    const int group_tok0 = rg * NT * TQ;
+    const bool has_rows = group_tok0 < it.q_ntok;
+    const int pos_first = it.pos0 + min(group_tok0, it.q_ntok - 1);
+    const int pos_last = it.pos0 + min(group_tok0 + NT * TQ, it.q_ntok) - 1;   // nothing beyond is seen by any row of the group
 
     f32x4_t o[NT][DT], lacc[NT];
     float m[NT];
@@ -370,82 +481,115 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
         for (int dt = 0; dt < DT; dt++) o[nt][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);
-    const uint32_t page_bytes = (uint32_t)a.n_kv * 2 * 16 * D * 2, lane16 = lane * 16;
-    // block c = wave KS + k of a pair: k-step c / 4, K or V by the second bit of c, page a or b by the first
-    const uint8_t* const pool_wave = reinterpret_cast<const uint8_t*>(a.pool_slot) + (size_t)it.kv_head * 2 * 16 * D * 2 + (wave * KS >> 2) * 1024 +
-                                     (KS == 4 ? 0 : (wave & 1) * 32 * D);
+    const uint32_t page_bytes = (uint32_t)a.n_kv * 2 * 16 * D * 2, lane16 = lane * 16, vswap = lane & 8;
+    // A pair is 4 KS KiB blocks [k-step][K page a, K page b, V page a, V page b]; the wavefront copies the blocks LPW wave + k.
+    const int c0 = wave * LPW;
+    const uint8_t* const pool_wave = reinterpret_cast<const uint8_t*>(a.pool_slot) + (size_t)it.kv_head * 2 * 16 * D * 2 + (c0 >> 2) * 1024 + ((c0 >> 1) & 1) * 32 * D;
     const uint32_t ring0 = (uint32_t)(uintptr_t)ring;
 
     const int n_pg = it.page_end - it.page_begin, n_pairs = (n_pg + 1) >> 1, pair0 = it.page_begin >> 1;
+    const int n_rounds = (n_pairs + KW - 1) / KW;
     int tb0 = 0;   // ids of 64 pages at a time, lane l holding page tb0 + l of the item's range
     int tbl = pages[it.page_begin + min(lane, n_pg - 1)];
-    auto issue = [&](int j, int slot) {
-        const int jj = min(j, n_pairs - 1);
-        if (2 * jj >= tb0 + 64) {
+    auto issue = [&](int round) {
+        const int first = min(round * KW, n_pairs - 1);
+        if (2 * first >= tb0 + 64) {   // a round lies within 64 pages
             tb0 += 64;
             tbl = pages[it.page_begin + tb0 + min(lane, n_pg - tb0 - 1)];
             vm_wait<0>();   // here, so that the compiler does not wait for everything where the paths join
         }
-        const int la = 2 * jj - tb0;
-        const uint32_t pa = __builtin_amdgcn_readlane(tbl, la);
-        const uint32_t pb = __builtin_amdgcn_readlane(tbl, min(la + 1, n_pg - tb0 - 1));
-        const uint8_t* ca = pool_wave + (uint64_t)pa * page_bytes;
-        const uint8_t* cb = pool_wave + (uint64_t)pb * page_bytes;
-        uint8_t* dst = ring + slot * PAIR_BYTES + wave * (KS * 1024);
-        uint32_t off[2] = {lane16, lane16 + (KS == 4 ? 32 * D : 0)};   // K and V of a page (of head dim 64, a wavefront copies only one)
-        asm volatile("" : "+v"(off[0]), "+v"(off[1]));   // 32-bit offsets in registers of their own: scalar base + vector offset addressing
 #pragma unroll
-        for (int k = 0; k < KS; k++) PS_GLOBAL_TO_LDS(((k & 1) ? cb : ca) + off[k >> 1], dst + k * 1024);
+        for (int j = 0; j < KW; j++) {
+            const int la = 2 * min(round * KW + j, n_pairs - 1) - tb0;
+            uint8_t* dst = ring + ((round % ROUNDS) * KW + j) * PAIR_BYTES + c0 * 1024;
+            const uint32_t page[2] = {(uint32_t)__builtin_amdgcn_readlane(tbl, la), (uint32_t)__builtin_amdgcn_readlane(tbl, min(la + 1, n_pg - tb0 - 1))};
+            uint32_t off[2] = {lane16, lane16 + 32 * D};   // K and V of a page (of head dim 64, a wavefront copies only one)
+            asm volatile("" : "+v"(off[0]), "+v"(off[1]));   // 32-bit offsets in registers of their own: scalar base + vector offset addressing
+            const uint8_t* src[2] = {pool_wave + (uint64_t)page[0] * page_bytes, pool_wave + (uint64_t)page[1] * page_bytes};
+#pragma unroll
+            for (int k = 0; k < LPW; k++) {
+                if constexpr (ONCE) global_to_lds_stream(src[k & 1] + off[k >> 1], dst + k * 1024);
+                else PS_GLOBAL_TO_LDS(src[k & 1] + off[k >> 1], dst + k * 1024);
+            }
+        }
     };
 
     __builtin_amdgcn_s_barrier();   // every wavefront has finished with the ring (previous item)
-    issue(0, 0);
-    issue(1, 1);
-    // The wavefront computes on the pairs that begin at or before its last position, first those without a mask, and only keeps copying
-    // and meeting the barriers for the rest: three loops, so that no accumulator is live across a branch.
-    const int n_mine = !wave_has_rows ? 0 : max(0, min(n_pairs, (pos_last >> 5) - pair0 + 1));
+#pragma unroll
+    for (int k = 0; k < ROUNDS - 1; k++) issue(k);
+    // The row group sees the first n_mine pairs, the first n_free of them without a mask; of both the wavefront has every KW-th.  Past
+    // them it only keeps copying and meeting the barriers: three loops, so that no accumulator is live across a branch.
+    const int n_mine = !has_rows ? 0 : max(0, min(n_pairs, (pos_last >> 5) - pair0 + 1));
     const int n_free = max(0, min(n_mine, first_masked_pair(it, pos_first) - pair0));
-    int slot = 0;
-    auto step = [&](int i) {
-        vm_wait<KS>();
-        __builtin_amdgcn_s_barrier();
-        issue(i + 2, slot >= 1 ? slot - 1 : TREE_RING - 1);     // (i + 2) % 3
-    };
-    auto next = [&]() { slot = slot + 1 == TREE_RING ? 0 : slot + 1; };
-    uint32_t word[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++) word[nt] = 0;
+    const int free_rounds = (n_free - kg + KW - 1) / KW, my_rounds = (n_mine - kg + KW - 1) / KW;   // of less than one pair: 0 or less
+    bool specials = false;
     int i = 0;
-    for (; i < n_free; i++) {
-        step(i);
-        team_pair<D, NT, false>(o, lacc, m, ring0 + slot * PAIR_BYTES + lane * 16, qf, word, g, scale2);
-        next();
+    auto step = [&]() {
+        vm_wait<(ROUNDS - 2) * KW * LPW>();
+        __builtin_amdgcn_s_barrier();
+        issue(i + ROUNDS - 1);
+    };
+    auto slot = [&]() { return ring0 + ((i % ROUNDS) * KW + kg) * PAIR_BYTES + lane16; };
+    for (; i < free_rounds; i++) {
+        step();
+        team_pair<D, G, NT, false>(o, lacc, m, specials, slot(), qf, a, it, tok_row, 0, g, vswap, scale2);
     }
-    for (; i < n_mine; i++) {
-        step(i);
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++) word[nt] = visible_word(a, it, min(tok_row + nt * TQ, it.q_ntok - 1), pair0 + i);
-        team_pair<D, NT, true>(o, lacc, m, ring0 + slot * PAIR_BYTES + lane * 16, qf, word, g, scale2);
-        next();
+    if (NT == 3 && i < my_rounds) {
+        // Read once more: the masked loop needs more registers than there are beside three tiles, and queries that live through both
+        // loops would be the ones it moves out, in the long loop too.
+        int tok = tok_row;
+        asm volatile("" : "+v"(tok));
+        load_queries(tok);
     }
-    for (; i < n_pairs; i++) {
-        step(i);
-        next();
+    for (; i < my_rounds; i++) {
+        step();
+        team_pair<D, G, NT, true>(o, lacc, m, specials, slot(), qf, a, it, tok_row, pair0 + i * KW + kg, g, vswap, scale2);
     }
+    for (; i < n_rounds; i++) step();
     vm_wait<0>();   // the surplus copies have landed before the ring is used again
-    if (!wave_has_rows) return;
+    if constexpr (KW > 1) {
+        // Key groups 1 .. leave maximum, sum and accumulators in LDS, group 0 joins them.
+        __builtin_amdgcn_s_barrier();   // nobody reads or fills the ring any more
+        float4* const mine = reinterpret_cast<float4*>(ring + (size_t)(kg * RW + rg) * (DT + 1) * 1024);
+        if (kg > 0) {
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) mine[dt * 64 + lane] = float4{o[0][dt][0], o[0][dt][1], o[0][dt][2], o[0][dt][3]};
+            mine[DT * 64 + lane] = float4{m[0], lacc[0][0], specials ? 1.f : 0.f, 0.f};
+        }
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int j = 1; j < KW; j++) {
+            const float4* theirs = mine + (size_t)j * RW * (DT + 1) * 64;
+            const float4 ml = theirs[DT * 64 + lane];
+            const float M = fmaxf(m[0], ml.x), ms = rounded_product(M, scale2);
+            const float f = __builtin_amdgcn_exp2f(rounded_product(m[0], scale2) - ms), h = __builtin_amdgcn_exp2f(rounded_product(ml.x, scale2) - ms);
+            m[0] = M;
+            lacc[0][0] = lacc[0][0] * f + ml.y * h;
+            specials = specials || __builtin_amdgcn_ballot_w64(ml.z != 0.f) != 0;
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) {
+                const float4 v = theirs[dt * 64 + lane];
+                o[0][dt][0] = o[0][dt][0] * f + v.x * h; o[0][dt][1] = o[0][dt][1] * f + v.y * h;
+                o[0][dt][2] = o[0][dt][2] * f + v.z * h; o[0][dt][3] = o[0][dt][3] * f + v.w * h;
+            }
+        }
+    }
+    if (!has_rows) return;
     float l[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
         l[nt] = lacc[nt][0];
         m[nt] = rounded_product(m[nt], scale2);   // the merge works in the exponent's units
     }
-    store_rows<D, G, NT>(a, it, o, m, l, tok_row, wave * NT, lane);
+    store_rows<D, G, NT, true>(a, it, o, m, l, tok_row, rg * NT, lane);
+    if (specials) add_specials<D, G, NT>(a, it, tok_row, rg * NT, pair0 + n_free, pair0 + n_mine - 1, lane);
 }
 
-template <int D, int G, int NT>
+// ONCE: no sequence has a second query block that reads the same pages again.
+template <int D, int G, bool ONCE>
 __global__ __launch_bounds__(64 * TREE_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_kernel(TreeArgs a) {
-    __shared__ __attribute__((aligned(1024))) uint8_t ring[TREE_RING * (D / 8) * 1024];
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[TREE_RING * (D / 8) * 1024];   // also holds the join: 4 (D / 16 + 1) KiB
     // contiguous shares of either work list on every XCD, as in attn_kernel
     const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -453,7 +597,14 @@ __global__ __launch_bounds__(64 * TREE_WAVES) __attribute__((amdgpu_waves_per_eu
         const int t = xcd * a.team_per_xcd + j;
         if (t >= a.n_team) return;
         const int i0 = a.worker_begin[t], i1 = a.worker_begin[t + 1];
-        for (int i = i0; i < i1; i++) team_item<D, G, NT>(a, a.items[i], ring, wave);
+        for (int i = i0; i < i1; i++) {
+            const AttnItem it = a.items[i];
+            const int tiles = (it.q_ntok + 16 / G - 1) / (16 / G);
+            if (tiles <= 2) team_item<D, G, 1, 2, ONCE>(a, it, ring, wave);
+            else if (tiles <= 4) team_item<D, G, 1, 1, ONCE>(a, it, ring, wave);
+            else if (tiles <= 8) team_item<D, G, 2, 1, ONCE>(a, it, ring, wave);
+            else team_item<D, G, 3, 1, ONCE>(a, it, ring, wave);
+        }
     } else {
         const int w = a.n_team + (xcd * a.wave_blocks_per_xcd + (j - a.team_per_xcd)) * TREE_WAVES + wave;
         if (j - a.team_per_xcd >= a.wave_blocks_per_xcd || w >= a.n_workers) return;
@@ -532,13 +683,13 @@ __global__ __launch_bounds__(64 * MERGE_MAX_WAVES) void tree_merge_kernel(TreeAr
             uint2 w;
             w.x = pack_bf16(acc.x * inv, acc.y * inv);
             w.y = pack_bf16(acc.z * inv, acc.w * inv);
-            *reinterpret_cast<uint2*>(a.out + (a.ldo ? (size_t)tok * a.ldo + head * D + col : act_offset(tok, head * D + col, a.n_q * D))) = w;
+            *reinterpret_cast<uint2*>(out_at(a, tok, head * D + col)) = w;
         }
         if (NWS > 1) __syncthreads();  // the next pass overwrites the LDS slots
     }
 }
 
-int tree_tokens_per_item(int G, int nt) { return TREE_WAVES * nt * (16 / G); }
+int tree_tokens_per_item(int G) { return TREE_WAVES * TREE_NT * (16 / G); }
 
 template <int D, int G>
 static hipError_t launch_dg(const TreeArgs& a_in, hipStream_t st) {
@@ -547,10 +698,8 @@ static hipError_t launch_dg(const TreeArgs& a_in, hipStream_t st) {
     a.wave_blocks_per_xcd = ((a.n_workers - a.n_team + TREE_WAVES - 1) / TREE_WAVES + 7) >> 3;
     const dim3 grid((a.team_per_xcd + a.wave_blocks_per_xcd) * 8), block(64 * TREE_WAVES);
     if (a.ev_begin) (void)hipEventRecord(a.ev_begin, st);
-    switch (a.nt) {
-        case 3: hipLaunchKernelGGL((tree_kernel<D, G, 3>), grid, block, 0, st, a); break;
-        default: return hipErrorInvalidValue;
-    }
+    if (a.pages_once) hipLaunchKernelGGL((tree_kernel<D, G, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((tree_kernel<D, G, false>), grid, block, 0, st, a);
     hipError_t e = hipGetLastError();
     if (a.ev_end) (void)hipEventRecord(a.ev_end, st);
     if (e != hipSuccess || a.n_groups == 0) return e;
