@@ -98,6 +98,10 @@ extern "C" ps_status ps_create(const ps_model_desc* desc, void* hip_stream, ps_c
     hipError_t e = hipMemcpy(c->rope_cs, cs.data(), cs.size() * sizeof(float), hipMemcpyHostToDevice);
     if (e != hipSuccess) { ps_destroy(c); return hip_fail(nullptr, e, "hipMemcpy(rotary table)"); }
     c->worker_slots = attention_worker_slots();
+    st = dev_alloc(nullptr, &c->ws_pick, PICK_WORKSPACE_BYTES, "partial picks");
+    if (st != PS_OK) { ps_destroy(c); return st; }
+    e = hipMemset(c->ws_pick, 0, PICK_WORKSPACE_BYTES);
+    if (e != hipSuccess) { ps_destroy(c); return hip_fail(nullptr, e, "hipMemset(partial picks)"); }
     {   // set-up for ps_step_static, so that the entry point itself never allocates
         int dev = 0;
         e = hipGetDevice(&dev);
@@ -153,7 +157,7 @@ extern "C" void ps_destroy(ps_ctx* c) {
         dev_free(c->rope_cs);
         dev_free(c->pool);
         free_workspaces(c);
-        dev_free(c->embedding); dev_free(c->g_final); dev_free(c->wout_t); dev_free(c->ws_logits); dev_free(c->ws_next);
+        dev_free(c->embedding); dev_free(c->g_final); dev_free(c->wout_t); dev_free(c->ws_logits); dev_free(c->ws_next); dev_free(c->ws_pick);
         for (auto& e : c->ev_head) if (e) (void)hipEventDestroy(e);
         dev_free(c->part_o); dev_free(c->part_ml);
         dev_free(c->ws_skfrag); dev_free(c->ws_skcnt);

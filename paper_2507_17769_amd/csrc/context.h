@@ -108,6 +108,7 @@ struct ps_ctx {
     size_t logits_bytes = 0;
     int32_t* ws_next = nullptr;   // [cap] greedy tokens when the caller passes none
     int next_cap = 0;
+    void* ws_pick = nullptr;      // see launch_pick: of fixed size, so that the call never allocates
     hipEvent_t ev_head[4] = {nullptr, nullptr, nullptr, nullptr};
     float* ws_part = nullptr;  // fp32 GEMM partials [splits][T][N], shared by the three projections
     size_t part_bytes = 0;

@@ -219,7 +219,11 @@ struct PickArgs {
     int32_t* next;           // or null
     float* logprob;          // or null
 };
-hipError_t launch_pick(const PickArgs& a, hipStream_t st);
+// workspace: PICK_WORKSPACE_BYTES of device memory.  Behind the partial picks lies a counter a row, each in a line of its own: atomics on one line
+// from all over the device wait for one another.  They are zero before the first launch, and every launch leaves them so.
+constexpr int PICK_PARTIALS = 65536, PICK_MAX_ROWS = 4096, PICK_LINE = 32;
+constexpr size_t PICK_WORKSPACE_BYTES = (size_t)PICK_PARTIALS * 16 + (size_t)PICK_MAX_ROWS * PICK_LINE * 4;
+hipError_t launch_pick(const PickArgs& a, void* workspace, hipStream_t st);
 
 int attention_worker_slots();  // wavefronts of the attention kernel that are resident at once on this device
 

@@ -361,7 +361,7 @@ extern "C" ps_status ps_pick_tokens(ps_ctx* c, const void* logits, int32_t dtype
         a.rules = *rules;
     }
     OnDevice on(c);
-    HIP_TRY(c, launch_pick(a, c->stream));
+    HIP_TRY(c, launch_pick(a, c->ws_pick, c->stream));
     return PS_OK;
 }
 
@@ -438,7 +438,7 @@ extern "C" ps_status ps_verify_tokens(ps_ctx* c, const ps_tree* tree, const int3
             a.rules = *rules;
             if (rules->n_lists) { a.rules.row_list = t->row_seq; a.rules.row_token = t->dev_tokens; a.rules.row_prev = t->row_prev; }
         }
-        if (a.out || a.next || a.logprob) HIP_TRY(c, launch_pick(a, c->stream));
+        if (a.out || a.next || a.logprob) HIP_TRY(c, launch_pick(a, c->ws_pick, c->stream));
         return PS_OK;
     });
 }
