@@ -130,8 +130,6 @@ struct Quad {
         }
     }
 };
-// Arithmetic on x stays behind this point, out of the branch that loads it.
-__device__ __forceinline__ void hold(int& x) { asm volatile("" : "+v"(x)); }
 
 // grid (segments * groups of rows): the first segments of all rows, where vocabularies keep their frequent tokens, start first.  Q quads of adjacent tokens a thread: a segment is 1024 Q tokens.
 template <bool BF16, int Q, bool WIDE>

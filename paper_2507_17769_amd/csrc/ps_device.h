@@ -34,6 +34,9 @@ __device__ __forceinline__ uint4 ldg16_stream(const void* p) {
 
 __device__ __forceinline__ float silu_f(float z) { return z / (1.0f + __expf(-z)); }
 
+// Arithmetic on x stays behind this point: moved into the branch that loads x, it would be a wait for each such load on its own.
+__device__ __forceinline__ void hold(int& x) { asm volatile("" : "+v"(x)); }
+
 // Sum over the wavefront: rotations within each row of 16 lanes (DPP, no trip through LDS as a shuffle takes), then the four rows.
 __device__ __forceinline__ float wave_sum(float v) {
     const auto ror = [](float x, auto n) {
