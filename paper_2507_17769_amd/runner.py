@@ -28,11 +28,21 @@ class _PoolMemory:
         self.__cuda_array_interface__ = {"shape": (n_bytes // 2,), "typestr": "<i2", "data": (address, False), "version": 3}
 
 
+_DTYPE_CODES = {torch.float32: B.PS_F32, torch.bfloat16: B.PS_BF16}
+
+
 def _dtype_code(t):
-    codes = {torch.float32: B.PS_F32, torch.bfloat16: B.PS_BF16}
-    if t.dtype not in codes:
+    if t.dtype not in _DTYPE_CODES:
         raise TypeError(f"expected a float32 or bfloat16 tensor, not {t.dtype}")
-    return codes[t.dtype]
+    return _DTYPE_CODES[t.dtype]
+
+
+# The tensors of ps_logit_rules: those with an entry per list, those of offsets (one more), those with an entry per row.
+_RULE_TYPES = {n: torch.float32 if n in ("repetition", "frequency", "presence", "bias_value") else torch.int32
+               for n, t in B.ps_logit_rules._fields_ if t is C.c_void_p}
+_RULE_LISTS = ("repetition", "frequency", "presence", "output_begin", "history_begin", "bias_begin")
+_RULE_BEGINS = ("history_begin", "bias_begin")
+_RULE_ROWS = ("mask_row", "row_list", "row_token", "row_prev")
 
 
 class Engine:
@@ -131,11 +141,16 @@ class Engine:
             raise ValueError(f"{name} is on {t.device}, the engine on {self.device}")
         if t.dtype not in dtypes:
             raise TypeError(f"{name} has type {t.dtype}")
-        if t.dim() < 2 or t.shape[0] != n_rows or t[:1].numel() != (width if n_rows else 0):
-            raise ValueError(f"{name} must hold {n_rows} rows of {width}, not {tuple(t.shape)}")
-        if n_rows and not t[0].is_contiguous():
+        shape, stride = t.shape, t.stride()
+        n, adjacent = 1, True
+        for size, step in zip(shape[:0:-1], stride[:0:-1]):
+            adjacent = adjacent and (size == 1 or step == n)
+            n *= size
+        if len(shape) < 2 or shape[0] != n_rows or (n_rows and n != width):
+            raise ValueError(f"{name} must hold {n_rows} rows of {width}, not {tuple(shape)}")
+        if n_rows and not adjacent:
             raise ValueError(f"the elements of a row of {name} must be adjacent")
-        return t.data_ptr(), (t.stride(0) if n_rows > 1 else max(width, t.stride(0)))
+        return t.data_ptr(), (stride[0] if n_rows > 1 else max(width, stride[0]))
 
     def kv_pool(self):
         """The KV pool as a bf16 tensor [KV slot][page][kv head][K, V][16 * head_dim] (a view: see ps_kv_pool for the order of a
@@ -188,39 +203,40 @@ class Engine:
 
     def _rules(self, rules, n_rows):
         """rules: dict of device tensors with the names of ps_logit_rules ("mask" int32 [n_masks][words])."""
-        r = B.ps_logit_rules()
-        floats = ("repetition", "frequency", "presence", "bias_value")
-        known = {n for n, t in B.ps_logit_rules._fields_ if t is C.c_void_p}
+        r, device, size = B.ps_logit_rules(), self.device, {}
         for name, t in rules.items():
-            if name not in known:
+            dtype = _RULE_TYPES.get(name)
+            if dtype is None:
                 raise ValueError(f"unknown rule {name}")
             if t is None:
                 continue
-            if t.device != self.device or t.dtype != (torch.float32 if name in floats else torch.int32):
-                raise TypeError(f"{name} must be a {'float32' if name in floats else 'int32'} tensor of the engine's device")
-            if name != "mask" and (t.dim() != 1 or not t.is_contiguous()):
-                raise ValueError(f"{name} must be one contiguous row")
-            if name == "mask" and (t.dim() != 2 or (t.numel() and t.stride(1) != 1)):
+            if t.dtype != dtype or t.device != device:
+                raise TypeError(f"{name} must be a {str(dtype)[6:]} tensor of the engine's device")
+            n = t.numel()
+            if name != "mask":
+                if t.dim() != 1 or not t.is_contiguous():
+                    raise ValueError(f"{name} must be one contiguous row")
+                size[name] = n
+            elif t.dim() != 2 or (n and t.stride(1) != 1):
                 raise ValueError("mask must hold rows of adjacent words")
-            if t.numel():
+            if n:
                 setattr(r, name, t.data_ptr())
-        got = {k: t for k, t in rules.items() if t is not None}
-        lists = {k: got[k].shape[0] for k in ("repetition", "frequency", "presence", "output_begin") if k in got}
-        lists.update({k: got[k].shape[0] - 1 for k in ("history_begin", "bias_begin") if k in got})
+        lists = {k: size[k] - (k in _RULE_BEGINS) for k in _RULE_LISTS if k in size}
         if len(set(lists.values())) > 1:
             raise ValueError(f"the rules disagree about the number of lists: {lists}")
         r.n_lists = next(iter(lists.values()), 0)
-        r.n_history = got["history"].shape[0] if "history" in got else 0
-        r.n_biases = got["bias_token"].shape[0] if "bias_token" in got else 0
+        r.n_history = size.get("history", 0)
+        r.n_biases = size.get("bias_token", 0)
         if r.n_history == 0:
             r.history = r.output_begin = None
-        if "bias_token" in got and ("bias_value" not in got or got["bias_value"].shape != got["bias_token"].shape):
+        if "bias_token" in size and size.get("bias_value") != size["bias_token"]:
             raise ValueError("bias_value must hold one value per bias_token")
-        for name in ("mask_row", "row_list", "row_token", "row_prev"):
-            if name in got and got[name].shape[0] != n_rows:
+        for name in _RULE_ROWS:
+            if size.get(name, n_rows) != n_rows:
                 raise ValueError(f"{name} must hold one entry per row")
         if r.mask:
-            r.n_masks, r.mask_stride = got["mask"].shape[0], max(got["mask"].shape[1], got["mask"].stride(0))
+            mask = rules["mask"]
+            r.n_masks, r.mask_stride = mask.shape[0], max(mask.shape[1], mask.stride(0))
         else:
             r.mask_row = None
         return r
