@@ -151,24 +151,30 @@ __device__ __forceinline__ void hide(f32x4_t& sa, f32x4_t& sb, uint32_t word, in
     }
 }
 
-// Softmax of one tile for a pair: raw scores -> P as a packed operand, running maximum m (in the scores' units) and the factor
-// alpha of what came before.  The row sums are taken from the rounded P by the matrix unit, so that the weights of a row add up
-// to one exactly as rounded; the maximum is exact, so a row's largest weight carries no rounding.
-__device__ __forceinline__ bf16x8_t tile_softmax(const f32x4_t& sa, const f32x4_t& sb, float& m, float& alpha, float scale2) {
+// Softmax of one tile for a pair: raw scores -> P as a packed operand, 2^(s scale2 - m).  m is a reference, not the running maximum: any
+// number cancels that is the same in a row's sum and products, so it follows the maximum only when that has outgrown it by 2^16 (fp32 sums
+// have room for far more).  After an item's first pairs that hardly ever happens, and a pair then needs neither the maximum across the four
+// lanes of a row nor what came before rescaled, which took a third of the loop's vector instructions.  The row sums are taken from the
+// rounded P by the matrix unit, so that the weights of a row add up to one exactly as rounded.
+constexpr float OUTGROWN = 16.f;
+template <int DT>
+__device__ __forceinline__ bf16x8_t tile_softmax(const f32x4_t& sa, const f32x4_t& sb, float& m, f32x4_t (&o)[DT], f32x4_t& l, float scale2) {
     const float sv[8] = {sa[0], sa[1], sa[2], sa[3], sb[0], sb[1], sb[2], sb[3]};
-    float mx = max3(max3(sv[0], sv[1], sv[2]), max3(sv[3], sv[4], sv[5]), max3(sv[6], sv[7], m));
-    {
+    float mx = max3(max3(sv[0], sv[1], sv[2]), max3(sv[3], sv[4], sv[5]), max3(sv[6], sv[7], sv[7]));
+    if (__builtin_amdgcn_ballot_w64(fmaf(mx, scale2, -m) > OUTGROWN) != 0) {
         const u32x2_t x = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         const float y = max3(__uint_as_float(x.x), __uint_as_float(x.y), mx);
         const u32x2_t z = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
         mx = max3(__uint_as_float(z.x), __uint_as_float(z.y), y);
+        const float ms = fmaxf(rounded_product(mx, scale2), m), alpha = __builtin_amdgcn_exp2f(m - ms);
+        m = ms;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) { o[dt][0] *= alpha; o[dt][1] *= alpha; o[dt][2] *= alpha; o[dt][3] *= alpha; }
+        l[0] *= alpha; l[1] *= alpha; l[2] *= alpha; l[3] *= alpha;
     }
-    const float ms = rounded_product(mx, scale2);
-    alpha = __builtin_amdgcn_exp2f(rounded_product(m, scale2) - ms);
-    m = mx;
     float pv[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) pv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], scale2, -ms));
+    for (int i = 0; i < 8; i++) pv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], scale2, -m));
     uint4 pw;
     pw.x = pack_bf16(pv[0], pv[1]);
     pw.y = pack_bf16(pv[2], pv[3]);
@@ -187,15 +193,6 @@ __device__ __forceinline__ void matrix_results(f32x4_t& a, f32x4_t& b, f32x4_t& 
 }
 
 constexpr u32x4_t ONES = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-
-// What came before is rescaled; once the running maximum has settled alpha is exactly 1 in every lane and nothing is done.
-template <int DT>
-__device__ __forceinline__ void rescale(f32x4_t (&o)[DT], f32x4_t& l, float alpha) {
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) == 0) return;
-#pragma unroll
-    for (int dt = 0; dt < DT; dt++) { o[dt][0] *= alpha; o[dt][1] *= alpha; o[dt][2] *= alpha; o[dt][3] *= alpha; }
-    l[0] *= alpha; l[1] *= alpha; l[2] *= alpha; l[3] *= alpha;
-}
 
 // End of an item: the NT tiles of a wavefront go to the output (normalised) or, for an item that covers only part of its KV span, to
 // partial slots it.partial + slot0 + nt.  l: each row's sum, the same in the four lanes that share the row.  Padding gets zeros.
@@ -267,9 +264,7 @@ __device__ __forceinline__ void wave_pair(f32x4_t (&o)[1][D / 16], f32x4_t& lacc
             }
         }
     }
-    float alpha;
-    const bf16x8_t pf = tile_softmax(sa, sb, m, alpha, scale2);
-    rescale<DT>(o[0], lacc, alpha);
+    const bf16x8_t pf = tile_softmax<DT>(sa, sb, m, o[0], lacc, scale2);
     lacc = mfma_16x16x32(ONES, pf, lacc);
     // one product per page and d-tile: each 8-byte half of a loaded register quad is an operand as it stands, where one for both pages would
     // take 64 register moves
@@ -340,7 +335,7 @@ __device__ __forceinline__ void wave_item(const TreeArgs& a, const AttnItem it) 
             for (int s = 0; s < KS; s++) { b0.ka[s] = b1.ka[s]; b0.kb[s] = b1.kb[s]; b0.va[s] = b1.va[s]; b0.vb[s] = b1.vb[s]; }
         }
     }
-    const float ml[1] = {rounded_product(m, scale2)}, l[1] = {lacc[0]};
+    const float ml[1] = {m}, l[1] = {lacc[0]};
     store_rows<D, G, 1, false>(a, it, o, ml, l, r / G, 0, lane);
     if (specials) add_specials<D, G, 1>(a, it, r / G, 0, max(masked, it.page_begin >> 1), (it.page_end - 1) >> 1, lane);
 }
@@ -393,14 +388,13 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
     else if constexpr (NT == 2) matrix_results(sa[0], sb[0], sa[1], sb[1]);
     else matrix_results(sa[0], sb[0], sa[1], sb[1], sa[2], sb[2]);
     bf16x8_t pf[NT];
-    float alpha[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
         if constexpr (MASK) {
             hide(sa[nt], sb[nt], word[nt], g);
             __builtin_amdgcn_sched_barrier(0);
         }
-        pf[nt] = tile_softmax(sa[nt], sb[nt], m[nt], alpha[nt], scale2);
+        pf[nt] = tile_softmax<DT>(sa[nt], sb[nt], m[nt], o[nt], lacc[nt], scale2);
         if constexpr (MASK) __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (DT == 8)
@@ -424,7 +418,6 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
     __builtin_amdgcn_s_setprio(1);   // the matrix unit is fed first (see attn_kernel)
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-        rescale<DT>(o[nt], lacc[nt], alpha[nt]);
         lacc[nt] = mfma_16x16x32(ONES, pf[nt], lacc[nt]);
 #pragma unroll
         for (int dt = 0; dt < DT; dt++) {
@@ -562,8 +555,7 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
         for (int j = 1; j < KW; j++) {
             const float4* theirs = mine + (size_t)j * RW * (DT + 1) * 64;
             const float4 ml = theirs[DT * 64 + lane];
-            const float M = fmaxf(m[0], ml.x), ms = rounded_product(M, scale2);
-            const float f = __builtin_amdgcn_exp2f(rounded_product(m[0], scale2) - ms), h = __builtin_amdgcn_exp2f(rounded_product(ml.x, scale2) - ms);
+            const float M = fmaxf(m[0], ml.x), f = __builtin_amdgcn_exp2f(m[0] - M), h = __builtin_amdgcn_exp2f(ml.x - M);
             m[0] = M;
             lacc[0][0] = lacc[0][0] * f + ml.y * h;
             specials = specials || __builtin_amdgcn_ballot_w64(ml.z != 0.f) != 0;
@@ -578,10 +570,7 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
     if (!has_rows) return;
     float l[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-        l[nt] = lacc[nt][0];
-        m[nt] = rounded_product(m[nt], scale2);   // the merge works in the exponent's units
-    }
+    for (int nt = 0; nt < NT; nt++) l[nt] = lacc[nt][0];
     store_rows<D, G, NT, true>(a, it, o, m, l, tok_row, rg * NT, lane);
     if (specials) add_specials<D, G, NT>(a, it, tok_row, rg * NT, pair0 + n_free, pair0 + n_mine - 1, lane);
 }
