@@ -42,6 +42,15 @@ __device__ __forceinline__ uint32_t visible_word(const TreeArgs& a, const AttnIt
     const int left = it.pos0 + qc - 32 * pair;
     return left >= 31 ? 0xFFFFFFFFu : left < 0 ? 0u : (2u << left) - 1u;
 }
+// A team keeps the words of the first pairs that need them in LDS: a read from memory in the middle of the stream would wait for all the pages
+// on their way, 4 us a pair.
+constexpr int MASK_PAIRS = 4, MASK_ROWS = 16 * TREE_WAVES * TREE_NT;   // words of a row, tokens of a block at most
+__device__ __forceinline__ uint32_t team_word(const TreeArgs& a, const AttnItem& it, const uint32_t* kept, int qc, int pair) {
+    if (it.mask_at >= 0 && pair - it.mask_pair < MASK_PAIRS) return kept[(pair - it.mask_pair) * MASK_ROWS + qc];
+    int w = (int)visible_word(a, it, qc, pair);
+    hold(w);   // waited for here, not where the two ways meet
+    return (uint32_t)w;
+}
 // Padding sees nothing, not even itself.
 __device__ __forceinline__ bool is_padding(const TreeArgs& a, const AttnItem& it, int qc) {
     if (it.mask_at < 0) return false;
@@ -347,12 +356,12 @@ __device__ __forceinline__ void wave_item(const TreeArgs& a, const AttnItem it) 
 // one (vswap = 8), so accumulator dt holds in its rows 8 .. 15 the values of tile dt ^ 1: its lanes of g >= 2 (see dt_of).
 template <int D, int G, int NT, bool MASK>
 __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&lacc)[NT], float (&m)[NT], bool& specials, uint32_t addr, const bf16x8_t (&qf)[NT][D / 32],
-                                          const TreeArgs& a, const AttnItem& it, int tok_row, int pair, int g, uint32_t vswap, float scale2) {
+                                          const TreeArgs& a, const AttnItem& it, const uint32_t* kept, int tok_row, int pair, int g, uint32_t vswap, float scale2) {
     constexpr int KS = D / 32, DT = D / 16;
     uint32_t word[NT];
     if constexpr (MASK) {
 #pragma unroll
-        for (int nt = 0; nt < NT; nt++) word[nt] = visible_word(a, it, min(tok_row + nt * (16 / G), it.q_ntok - 1), pair);
+        for (int nt = 0; nt < NT; nt++) word[nt] = team_word(a, it, kept, min(tok_row + nt * (16 / G), it.q_ntok - 1), pair);
         __builtin_amdgcn_sched_barrier(0);
     }
     u32x4_t kk[2 * KS];
@@ -366,8 +375,7 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
     else
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(kk[0]), "+v"(kk[1]), "+v"(kk[2]), "+v"(kk[3]));
     f32x4_t sa[NT], sb[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
+    auto scores = [&](int nt) {
         sa[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         sb[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -375,6 +383,20 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
             sa[nt] = mfma_16x16x32(kk[2 * s], qf[nt][s], sa[nt]);
             sb[nt] = mfma_16x16x32(kk[2 * s + 1], qf[nt][s], sb[nt]);
         }
+    };
+    bf16x8_t pf[NT];
+    if constexpr (MASK) {   // tile by tile, for the registers
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            scores(nt);
+            matrix_results(sa[nt], sb[nt]);
+            hide(sa[nt], sb[nt], word[nt], g);
+            pf[nt] = tile_softmax<DT>(sa[nt], sb[nt], m[nt], o[nt], lacc[nt], scale2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) scores(nt);
     }
     __builtin_amdgcn_sched_barrier(0);   // the values after the keys: they take the keys' registers, and the softmax covers their way
     u32x2_t va[DT], vb[DT];
@@ -384,18 +406,12 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
         va[dt] = lds_read8(half, (4 * (dt >> 1) + 2) * 1024);
         vb[dt] = lds_read8(half, (4 * (dt >> 1) + 3) * 1024);
     }
-    if constexpr (NT == 1) matrix_results(sa[0], sb[0]);
-    else if constexpr (NT == 2) matrix_results(sa[0], sb[0], sa[1], sb[1]);
-    else matrix_results(sa[0], sb[0], sa[1], sb[1], sa[2], sb[2]);
-    bf16x8_t pf[NT];
+    if constexpr (!MASK) {
+        if constexpr (NT == 1) matrix_results(sa[0], sb[0]);
+        else if constexpr (NT == 2) matrix_results(sa[0], sb[0], sa[1], sb[1]);
+        else matrix_results(sa[0], sb[0], sa[1], sb[1], sa[2], sb[2]);
 #pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-        if constexpr (MASK) {
-            hide(sa[nt], sb[nt], word[nt], g);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        pf[nt] = tile_softmax<DT>(sa[nt], sb[nt], m[nt], o[nt], lacc[nt], scale2);
-        if constexpr (MASK) __builtin_amdgcn_sched_barrier(0);
+        for (int nt = 0; nt < NT; nt++) pf[nt] = tile_softmax<DT>(sa[nt], sb[nt], m[nt], o[nt], lacc[nt], scale2);
     }
     if constexpr (DT == 8)
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(va[0]), "+v"(va[1]), "+v"(va[2]), "+v"(va[3]), "+v"(va[4]), "+v"(va[5]), "+v"(va[6]), "+v"(va[7]),
@@ -435,7 +451,7 @@ __device__ __forceinline__ void team_pair(f32x4_t (&o)[NT][D / 16], f32x4_t (&la
 // the copies of the round that takes those slots, compute.  Past the item's last pair the copies fetch that pair again, into slots nobody
 // reads, so that the wait counts are the same in every trip.
 template <int D, int G, int NT, int KW, bool ONCE>
-__device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, uint8_t* ring, int wave) {
+__device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, uint8_t* ring, uint32_t* kept, int wave) {
     static_assert(KW == 1 || NT == 1, "the join holds one tile a wavefront");
     constexpr int KS = D / 32, DT = D / 16, TQ = 16 / G;
     constexpr int RW = TREE_WAVES / KW, ROUNDS = TREE_RING / KW;   // rounds in the ring
@@ -444,10 +460,13 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
     const int r = lane & 15, g = lane >> 4, rg = wave % RW, kg = wave / RW;
     const int32_t* pages = a.pages + it.page_off;
     const int head = it.kv_head * G + (r % G);
+    const int n_pg = it.page_end - it.page_begin;
+    int tbl = pages[it.page_begin + min(lane, n_pg - 1)];
 
     // Row (lane r) of tile nt is token (rg NT + nt) TQ + r / G of the block, clamped to the block's last token (rows past it
     // compute on that token's data and are not stored).
-    const int tok_row = rg * NT * TQ + r / G;
+    auto row_now = [&]() { return rg * NT * TQ + (lane_id() & 15) / G; };   // formed anew: not held through the loops
+    const int tok_row = row_now();
     bf16x8_t qf[NT][KS];
     auto load_queries = [&](int tok) {
 #pragma unroll
@@ -457,6 +476,14 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
 #pragma unroll
             for (int s = 0; s < KS; s++) qf[nt][s] = as_bf16x8(ldg16(qrow + 32 * s));
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int s = 0; s < KS; s++) {   // they have arrived: else their first use, in a loop, would wait in every trip, and with it for all copies
+                u32x4_t x = __builtin_bit_cast(u32x4_t, qf[nt][s]);
+                asm volatile("" : "+v"(x));
+                qf[nt][s] = __builtin_bit_cast(bf16x8_t, x);
+            }
     };
     load_queries(tok_row);
     const int group_tok0 = rg * NT * TQ;
@@ -480,10 +507,10 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
     const uint8_t* const pool_wave = reinterpret_cast<const uint8_t*>(a.pool_slot) + (size_t)it.kv_head * 2 * 16 * D * 2 + (c0 >> 2) * 1024 + ((c0 >> 1) & 1) * 32 * D;
     const uint32_t ring0 = (uint32_t)(uintptr_t)ring;
 
-    const int n_pg = it.page_end - it.page_begin, n_pairs = (n_pg + 1) >> 1, pair0 = it.page_begin >> 1;
+    const int n_pairs = (n_pg + 1) >> 1, pair0 = it.page_begin >> 1;
     const int n_rounds = (n_pairs + KW - 1) / KW;
-    int tb0 = 0;   // ids of 64 pages at a time, lane l holding page tb0 + l of the item's range
-    int tbl = pages[it.page_begin + min(lane, n_pg - 1)];
+    int tb0 = 0;   // ids of 64 pages at a time in tbl, lane l holding page tb0 + l of the item's range
+    hold(tbl);     // it has arrived: else every use of it in the loops would wait, and with it for all copies
     auto issue = [&](int round) {
         const int first = min(round * KW, n_pairs - 1);
         if (2 * first >= tb0 + 64) {   // a round lies within 64 pages
@@ -507,9 +534,24 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
         }
     };
 
-    __builtin_amdgcn_s_barrier();   // every wavefront has finished with the ring (previous item)
+    __builtin_amdgcn_s_barrier();   // every wavefront has finished with the ring and the words (previous item)
+    if (it.mask_at >= 0) {
+        const int qc = 64 * wave + lane, at = it.mask_at + min(qc, it.q_ntok - 1) * it.mask_words;
+        int w[MASK_PAIRS];
 #pragma unroll
-    for (int k = 0; k < ROUNDS - 1; k++) issue(k);
+        for (int k = 0; k < MASK_PAIRS; k++) w[k] = (int)a.masks[at + min(k, it.mask_words - 1)];
+#pragma unroll
+        for (int k = 0; k < ROUNDS - 1; k++) issue(k);
+#pragma unroll
+        for (int k = 0; k < MASK_PAIRS; k++) {
+            hold(w[k]);
+            if (qc < it.q_ntok) kept[k * MASK_ROWS + qc] = (uint32_t)w[k];   // read after the barrier of a round
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    } else {
+#pragma unroll
+        for (int k = 0; k < ROUNDS - 1; k++) issue(k);
+    }
     // The row group sees the first n_mine pairs, the first n_free of them without a mask; of both the wavefront has every KW-th.  Past
     // them it only keeps copying and meeting the barriers: three loops, so that no accumulator is live across a branch.
     const int n_mine = !has_rows ? 0 : max(0, min(n_pairs, (pos_last >> 5) - pair0 + 1));
@@ -525,18 +567,17 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
     auto slot = [&]() { return ring0 + ((i % ROUNDS) * KW + kg) * PAIR_BYTES + lane16; };
     for (; i < free_rounds; i++) {
         step();
-        team_pair<D, G, NT, false>(o, lacc, m, specials, slot(), qf, a, it, tok_row, 0, g, vswap, scale2);
+        team_pair<D, G, NT, false>(o, lacc, m, specials, slot(), qf, a, it, kept, tok_row, 0, g, vswap, scale2);
     }
     if (NT == 3 && i < my_rounds) {
         // Read once more: the masked loop needs more registers than there are beside three tiles, and queries that live through both
         // loops would be the ones it moves out, in the long loop too.
-        int tok = tok_row;
-        asm volatile("" : "+v"(tok));
-        load_queries(tok);
+        load_queries(row_now());
     }
+    const int mtok = row_now();
     for (; i < my_rounds; i++) {
         step();
-        team_pair<D, G, NT, true>(o, lacc, m, specials, slot(), qf, a, it, tok_row, pair0 + i * KW + kg, g, vswap, scale2);
+        team_pair<D, G, NT, true>(o, lacc, m, specials, slot(), qf, a, it, kept, mtok, pair0 + i * KW + kg, (lane_id() >> 4), vswap, scale2);
     }
     for (; i < n_rounds; i++) step();
     vm_wait<0>();   // the surplus copies have landed before the ring is used again
@@ -571,14 +612,15 @@ __device__ __forceinline__ void team_item(const TreeArgs& a, const AttnItem it, 
     float l[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) l[nt] = lacc[nt][0];
-    store_rows<D, G, NT, true>(a, it, o, m, l, tok_row, rg * NT, lane);
-    if (specials) add_specials<D, G, NT>(a, it, tok_row, rg * NT, pair0 + n_free, pair0 + n_mine - 1, lane);
+    store_rows<D, G, NT, true>(a, it, o, m, l, row_now(), rg * NT, lane_id());
+    if (specials) add_specials<D, G, NT>(a, it, row_now(), rg * NT, pair0 + n_free, pair0 + n_mine - 1, lane_id());
 }
 
 // ONCE: no sequence has a second query block that reads the same pages again.
 template <int D, int G, bool ONCE>
 __global__ __launch_bounds__(64 * TREE_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_kernel(TreeArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t ring[TREE_RING * (D / 8) * 1024];   // also holds the join: 4 (D / 16 + 1) KiB
+    __shared__ uint32_t kept[MASK_PAIRS * MASK_ROWS];                                       // words of masks (see team_word)
     // contiguous shares of either work list on every XCD, as in attn_kernel
     const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -589,10 +631,10 @@ __global__ __launch_bounds__(64 * TREE_WAVES) __attribute__((amdgpu_waves_per_eu
         for (int i = i0; i < i1; i++) {
             const AttnItem it = a.items[i];
             const int tiles = (it.q_ntok + 16 / G - 1) / (16 / G);
-            if (tiles <= 2) team_item<D, G, 1, 2, ONCE>(a, it, ring, wave);
-            else if (tiles <= 4) team_item<D, G, 1, 1, ONCE>(a, it, ring, wave);
-            else if (tiles <= 8) team_item<D, G, 2, 1, ONCE>(a, it, ring, wave);
-            else team_item<D, G, 3, 1, ONCE>(a, it, ring, wave);
+            if (tiles <= 2) team_item<D, G, 1, 2, ONCE>(a, it, ring, kept, wave);
+            else if (tiles <= 4) team_item<D, G, 1, 1, ONCE>(a, it, ring, kept, wave);
+            else if (tiles <= 8) team_item<D, G, 2, 1, ONCE>(a, it, ring, kept, wave);
+            else team_item<D, G, 3, 1, ONCE>(a, it, ring, kept, wave);
         }
     } else {
         const int w = a.n_team + (xcd * a.wave_blocks_per_xcd + (j - a.team_per_xcd)) * TREE_WAVES + wave;

@@ -10,6 +10,12 @@ static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 // the tiles of its query block.
 static int pair_weight(int tiles) { return tiles <= 4 ? 3 : tiles <= 8 ? 4 : 5; }
 
+// What a run takes besides its pairs, in pairs: to begin and to leave its rows (queries, page numbers and the first pages arrive, partials go),
+// and for each pair with a mask.  Measured as the ends of the workers: those of three runs ended half as late again as those of one when only
+// pairs were counted (126 us to 85 at 64-node trees of 64 heads).  START from 3 to 8 gives the same time to within 2%.
+constexpr int START = 4, MASKED = 2;
+constexpr int SHORT = 4;   // no cut leaves a run of fewer pairs
+
 constexpr int GANG = 4;   // query blocks that read the same pages at the same time, at most
 
 // The work list of the tree attention kernel, in the form that build_attention_plan gives a step's (AttnPlan): every (sequence, KV
@@ -28,7 +34,7 @@ static void build_tree_attention_plan(const PlanConfig& cfg, TreePlan& plan) {
     plan.two_blocks_per_cu = false;
     const int TQ = 16 / cfg.group, max_tiles = cfg.prefill_tokens / TQ;
 
-    struct Stream { int seq, q0, qb, blocks, qn, np, w; };   // `blocks` query blocks of qb tokens from token q0 on, qn tokens in all; pages
+    struct Stream { int seq, q0, qb, blocks, qn, np, w, free; };   // `blocks` query blocks of qb tokens from token q0 on, qn tokens in all; pages; pairs before the masks
     std::vector<Stream> pool[GANG + 1];                      // [0]: streaming wavefronts
     int64_t units[GANG + 1] = {}, pairs_team = 0, pairs_wave = 0;
     for (int s = 0; s < plan.n_seqs; s++) {
@@ -37,10 +43,10 @@ static void build_tree_attention_plan(const PlanConfig& cfg, TreePlan& plan) {
         const int gangs = ceil_div(ceil_div(sq.n_new, qb), GANG), per_gang = ceil_div(ceil_div(sq.n_new, qb), gangs);
         for (int q0 = 0; q0 < sq.n_new; q0 += per_gang * qb) {
             const int qn = std::min(per_gang * qb, sq.n_new - q0), n = ceil_div(qn, qb), c = tiles == 1 ? 0 : n;
-            const Stream st{s, q0, qb, n, qn, ceil_div(sq.kv_len - sq.n_new + q0 + qn, PS_PAGE_SIZE), c == 0 ? 1 : pair_weight(ceil_div(std::min(qb, qn), TQ))};
+            const Stream st{s, q0, qb, n, qn, ceil_div(sq.kv_len - sq.n_new + q0 + qn, PS_PAGE_SIZE), c == 0 ? 1 : pair_weight(ceil_div(std::min(qb, qn), TQ)), (sq.kv_len - sq.n_new + q0) / 32};
             pool[c].push_back(st);
             const int64_t pairs = (int64_t)ceil_div(st.np, 2) * cfg.n_kv_heads;
-            units[c] += pairs * st.w;
+            units[c] += (pairs + (int64_t)cfg.n_kv_heads * (START + MASKED * (ceil_div(st.np, 2) - st.free))) * st.w;
             (c == 0 ? pairs_wave : pairs_team) += pairs * n;
         }
     }
@@ -86,9 +92,11 @@ static void build_tree_attention_plan(const PlanConfig& cfg, TreePlan& plan) {
         const std::vector<Stream>& streams = pool[c];
         if (streams.empty()) continue;
         const int n = workers[c], width = std::max(1, c), base = (int)plan.worker_begin.size() - 1;
-        // Worker w ends where the cumulative weight reaches (w + 1) / n of it, so rounding to whole pairs never accumulates.  KV head
+        // Worker w ends where the cumulative weight reaches (w + 1) / n of it, to within SHORT pairs, so rounding never accumulates.  KV head
         // by head: the contiguous share of an XCD streams whole heads.
-        const int64_t total = units[c], part = total / n, rest = total % n;
+        int64_t total = units[c];
+        for (int i = 1; i < n; i++) total += START * streams[(size_t)i * streams.size() / n].w;   // of the runs that begin at a cut
+        const int64_t part = total / n, rest = total % n;
         auto boundary = [&](int w) { return part * (w + 1) + rest * (w + 1) / n; };
         runs.clear();
         slot.assign(streams.size() * cfg.n_kv_heads * width, -1);
@@ -100,15 +108,16 @@ static void build_tree_attention_plan(const PlanConfig& cfg, TreePlan& plan) {
                 const int n_pairs = ceil_div(st.np, 2);
                 int pair = 0, splits = 0;
                 while (pair < n_pairs) {
-                    const int64_t left = (w + 1 < n ? boundary(w) : total + st.w) - done;
-                    int take = (int)std::min<int64_t>(n_pairs - pair, left / st.w);
-                    if (take <= 0) {
-                        if (!runs.empty() && runs.back().worker == w) { w++; continue; }
-                        take = 1;   // a share smaller than one pair
-                    }
+                    const bool used = !runs.empty() && runs.back().worker == w;
+                    const int64_t left = (w + 1 < n ? boundary(w) : INT64_MAX / 2) - done;
+                    int take = (int)std::min<int64_t>(n_pairs - pair, left / st.w - START);
+                    if (take < std::min(SHORT, n_pairs - pair) && used) { w++; continue; }   // not worth beginning
+                    if (take < n_pairs - pair && n_pairs - pair - take < SHORT) take = n_pairs - pair;   // nor what would remain
+                    take = std::max(take, std::min(SHORT, n_pairs - pair));
                     runs.push_back(Run{w, (int)i, h, pair, take, splits++});
                     pair += take;
-                    done += (int64_t)take * st.w;
+                    done += (int64_t)(take + START) * st.w;
+                    if (pair == n_pairs) done += (int64_t)MASKED * (n_pairs - st.free) * st.w;
                     if (w + 1 < n && done >= boundary(w)) w++;
                 }
                 if (splits == 1) continue;
