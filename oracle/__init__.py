@@ -16,6 +16,8 @@ Modules
             and the seeded page allocator.
   layer     floating-point side: RMSNorm, RoPE, paged KV append, causal paged
             attention, SwiGLU feed-forward, one layer and a stack of layers.
+  tree      drafted tokens: trees, normalised heads, tree attention, rules on logits
+            and the pick, a verification step.
 
 Pins (tests/test_oracle_*.py): brute-force dense fp64 attention, torch's
 scaled_dot_product_attention / rms_norm / silu as library special cases,
