@@ -11,7 +11,7 @@
 //
 // Bounds and figures (16-bit cache, kernel alone, the join of partials beside it): eight chains of six, 32 query heads on 8 of 128, 80 MB: 21 + 4 us,
 // HBM takes 13.  16-node trees, 317 MB: 63 + 6 us for 52; a copy of the pages alone by the same ring takes 58.  64-node trees, 64 query heads, 330 MB
-// read by three query blocks each: 113 + 12 us, where the copies alone take 105 (the blocks' L2 requests) and the products alone 99; the
+// read by three query blocks each: 115 + 12 us, where the copies alone take 105 (the blocks' L2 requests) and the products alone 99; the
 // matrix unit is busy a third of the time.  A deeper ring, one block of eight wavefronts a compute unit, and P.V of one tile under the softmax
 // of the next were no faster.
 //
@@ -183,7 +183,8 @@ __device__ __forceinline__ bf16x8_t tile_softmax(const f32x4_t& sa, const f32x4_
         const float y = max3(__uint_as_float(x.x), __uint_as_float(x.y), mx);
         const u32x2_t z = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
         mx = max3(__uint_as_float(z.x), __uint_as_float(z.y), y);
-        const float ms = fmaxf(rounded_product(mx, scale2), m), alpha = __builtin_amdgcn_exp2f(m - ms);
+        // only the rows that have outgrown theirs: a row's roundings are its own affair, not that of the others in its tile
+        const float ms = fmaf(mx, scale2, -m) > OUTGROWN ? rounded_product(mx, scale2) : m, alpha = __builtin_amdgcn_exp2f(m - ms);
         m = ms;
 #pragma unroll
         for (int dt = 0; dt < DT; dt++) { o[dt][0] *= alpha; o[dt][1] *= alpha; o[dt][2] *= alpha; o[dt][3] *= alpha; }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2507_17769_amd.runner import Engine
-from test_gpu_tree import chain, check_picks, make_batch, make_engine, make_rules, pool_rows, rows_by_rules
+from test_gpu_tree import chain, check_picks, make_batch, make_engine, make_rules, pool_rows, random_tree, rows_by_rules
 
 pytestmark = pytest.mark.gpu
 
@@ -129,4 +129,27 @@ def test_picks_of_replays_and_of_calls_between_them():
             stream.synchronize()
             check_picks(captured, rows_by_rules(z.cpu().numpy(), r, V, 12))
             check_picks(got, other.cpu().numpy(), full=False)
+    eng.close()
+
+
+@pytest.mark.parametrize("n_q,n_kv,d", [(4, 2, 64), (32, 8, 128), (64, 8, 128)])
+@pytest.mark.parametrize("prefix,n", [(700, 3), (1500, 40), (40, 64)])
+def test_a_row_depends_on_no_other_rows_query(n_q, n_kv, d, prefix, n):
+    """To the bit: what the softmax of a tile does for one of its rows is not seen in another."""
+    rng = np.random.default_rng(prefix + n_q)
+    spec = [(prefix, random_tree(rng, n)), (prefix // 2, random_tree(rng, n))]
+    seqs, parents, pages, n_pages = make_batch(rng, spec)
+    eng = make_engine(n_q, n_kv, d, n_pages)
+    eng.kv_pool().normal_(generator=torch.Generator("cuda").manual_seed(1))
+    tree = eng.tree(seqs, parents)
+    q = torch.randn(2 * n, n_q, d, device="cuda", generator=torch.Generator("cuda").manual_seed(2)).to(torch.bfloat16)
+    loud = q.clone()
+    loud[::2] *= 40
+    nan = q.clone()
+    nan[::2] = float("nan")
+    out = [eng.tree_attention(0, tree, x) for x in (q, loud, nan)]
+    eng.ctx.sync()
+    assert torch.isfinite(out[0].float()).all()
+    assert torch.equal(out[0][1::2], out[1][1::2]) and torch.equal(out[0][1::2], out[2][1::2])
+    assert not torch.equal(out[0][::2], out[1][::2])
     eng.close()
