@@ -22,6 +22,7 @@
 #include "attention_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ps {
 
@@ -345,13 +346,16 @@ __device__ __forceinline__ void wave_item(const TreeArgs& a, const AttnItem it) 
             wave_pair<D, false>(o, lacc, m, specials, b1, qf, 0, g, scale2);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // the last one or two pairs of the prefix in the block, and the masked ones, which the stream ends with
-        for (; i < n_pairs; i++) {
+        // the last one or two pairs of the block that need no mask, whose values stay as they are, then the masked ones, which the stream ends with
+        auto step = [&](auto mask_c) {
+            constexpr bool MASK = decltype(mask_c)::value;
             load(b1, min(i + 1, n_pairs - 1));
-            wave_pair<D, true>(o, lacc, m, specials, b0, qf, pair0 + i < masked ? 0xFFFFFFFFu : visible_word(a, it, qc, pair0 + i), g, scale2);
+            wave_pair<D, MASK>(o, lacc, m, specials, b0, qf, MASK ? visible_word(a, it, qc, pair0 + i) : 0, g, scale2);
 #pragma unroll
             for (int s = 0; s < KS; s++) { b0.ka[s] = b1.ka[s]; b0.kb[s] = b1.kb[s]; b0.va[s] = b1.va[s]; b0.vb[s] = b1.vb[s]; }
-        }
+        };
+        for (; i < n_free; i++) step(std::false_type{});
+        for (; i < n_pairs; i++) step(std::true_type{});
     }
     const float ml[1] = {m}, l[1] = {lacc[0]};
     store_rows<D, G, 1, false>(a, it, o, ml, l, r / G, 0, lane);
