@@ -273,9 +273,10 @@ ps_status ps_step_tokens(ps_ctx* ctx, const ps_seq* seqs, int32_t n_seqs, const 
  * decode; a batch may mix all of them.
  *
  * A ps_tree holds what a batch of trees needs on the device (positions, slots, page lists, attention work list, masks, partial
- * sums): planned once, it serves all layers.  Except ps_tree_plan and the first ps_verify_tokens of a size, the calls below only launch
- * kernels, on the context's stream, and may be captured into a HIP graph; such a graph is valid until its tree is planned again or
- * destroyed, and is to be replayed in order with the context's other work, whose buffers it shares.  The calls may be made while another
+ * sums): planned once, it serves all layers.  ps_qk_norm_rope, ps_tree_attention, ps_tree_keep and ps_pick_tokens only launch kernels, on the context's
+ * stream, and may be captured into a HIP graph; such a graph is valid until its tree is planned again or destroyed or the pool replaced, and
+ * is to be replayed in order with the context's other work, whose buffers it shares.  ps_tree_plan, ps_init_qk_norm and ps_verify_tokens do work on the
+ * host that a replay would not repeat: PS_ESTATE, and nothing done, while the stream is captured.  The calls may be made while another
  * device is current. */
 typedef struct ps_tree ps_tree;
 
@@ -298,7 +299,7 @@ void ps_tree_destroy(ps_tree* tree);
  * attention output is zero.  Replaces what the tree held; work enqueued before still runs on that.  The arrays may be freed when the
  * call returns.  Device and pinned memory grows as needed (a larger batch than any before waits for the stream).  On a host-only context
  * only the host side is planned.  On an error the tree is empty.
- * Errors: PS_EINVAL / PS_ERANGE for a malformed batch or parent (not an earlier node, or padding), PS_ENOMEM. */
+ * Errors: PS_EINVAL / PS_ERANGE for a malformed batch or parent (not an earlier node, or padding), PS_ENOMEM, PS_ESTATE (no pool; captured). */
 ps_status ps_tree_plan(ps_ctx* ctx, ps_tree* tree, const ps_seq* seqs, int32_t n_seqs, const int32_t* parents);
 
 /* Integer side of the plan, host arrays as in ps_step_indices (positions: prefix + depth).  Errors: PS_EINVAL. */
@@ -306,7 +307,7 @@ ps_status ps_tree_indices(ps_ctx* ctx, const ps_tree* tree, int32_t* cu_seqlens,
 
 /* Gains of a layer whose queries and keys are normalised head by head before the rotation: device bf16 [head_dim] each, copied (the
  * caller may free them once ps_sync() has returned).  Both null: the layer does not normalise (the default).  All steps obey it.
- * Errors: PS_ERANGE (layer), PS_EINVAL (one null), PS_ENOMEM, PS_ESTATE (host-only context). */
+ * Errors: PS_ERANGE (layer), PS_EINVAL (one null), PS_ENOMEM, PS_ESTATE (host-only context; captured). */
 ps_status ps_init_qk_norm(ps_ctx* ctx, int32_t layer, const void* g_q, const void* g_k);
 
 /* A layer's projections -> rotated queries, and keys and values in the cache: for each query and key head u' = u * gain / sqrt(mean(u^2) +
@@ -369,7 +370,7 @@ ps_status ps_pick_tokens(ps_ctx* ctx, const void* logits, int32_t dtype, int64_t
  * over all T nodes.  token_ids: HOST [T].  rules (null: none): n_lists 0 or the batch's number of sequences, list s belonging to sequence s; row_list,
  * row_token and row_prev null (the nodes' branches count as output); mask_row and masks as for T rows.  Outputs, device, any may be null:
  * next_tokens int32 [T], logprobs fp32 [T], logits fp32 [T][vocab] (changed by the rules), hidden fp32 [T][hidden].  Rows of padding
- * hold numbers without meaning.  Errors: as ps_step_tokens and ps_pick_tokens; PS_ESTATE as ps_qk_norm_rope. */
+ * hold numbers without meaning.  Errors: as ps_step_tokens and ps_pick_tokens; PS_ESTATE as ps_qk_norm_rope, and while captured. */
 ps_status ps_verify_tokens(ps_ctx* ctx, const ps_tree* tree, const int32_t* token_ids, const ps_logit_rules* rules, int32_t* next_tokens,
                            float* logprobs, float* logits, float* hidden);
 

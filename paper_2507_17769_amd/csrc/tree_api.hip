@@ -106,6 +106,14 @@ ps_status check_tree(ps_ctx* c, const ps_tree* t, const char* name) {
     if (t->pool_id != c->pool_id) return fail(c, PS_ESTATE, std::string(name) + ": the KV pool was replaced after ps_tree_plan");
     return PS_OK;
 }
+// Calls whose host side a graph would not repeat (buffers that grow, pinned memory that later calls fill again, flags of the context).
+ps_status check_not_captured(ps_ctx* c, const char* name) {
+    hipStreamCaptureStatus now = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamIsCapturing(c->stream, &now);
+    if (e != hipSuccess) (void)hipGetLastError();   // the default stream while another one is captured
+    if (e != hipSuccess || now != hipStreamCaptureStatusNone) return fail(c, PS_ESTATE, std::string(name) + ": cannot be captured into a graph");
+    return PS_OK;
+}
 ps_status check_layer(ps_ctx* c, int32_t layer, const char* name) {
     if (layer < 0 || layer >= c->desc.n_layers) return fail(c, PS_ERANGE, std::string(name) + ": layer index out of range");
     return PS_OK;
@@ -225,8 +233,10 @@ extern "C" ps_status ps_tree_plan(ps_ctx* c, ps_tree* t, const ps_seq* seqs, int
         if (!c->host_only && !c->pool) return fail(c, PS_ESTATE, "ps_tree_plan: no KV pool (call ps_kv_alloc)");
         OnDevice on(c);
         std::string err;
+        ps_status st;
+        if (!c->host_only && (st = check_not_captured(c, "ps_tree_plan")) != PS_OK) return st;
         const PlanConfig pc = tree_plan_config(c);
-        ps_status st = validate_batch(seqs, n_seqs, pc, c->page_seen, err);
+        st = validate_batch(seqs, n_seqs, pc, c->page_seen, err);
         if (st == PS_OK) st = build_tree_plan(seqs, n_seqs, parents, pc, t->plan, err);
         if (st != PS_OK) return fail(c, st, "ps_tree_plan: " + err);
         t->args = TreeArgs{};
@@ -258,6 +268,7 @@ extern "C" ps_status ps_init_qk_norm(ps_ctx* c, int32_t layer, const void* g_q, 
     if (!g_q) { L.qk_norm = false; return PS_OK; }
     if (!aligned(g_q, 16) || !aligned(g_k, 16)) return fail(c, PS_EINVAL, "ps_init_qk_norm: gains must be 16-byte aligned");
     OnDevice on(c);
+    if ((st = check_not_captured(c, "ps_init_qk_norm")) != PS_OK) return st;
     const size_t bytes = (size_t)c->desc.head_dim * 2;
     if (!L.qk_gains && (st = dev_alloc(c, &L.qk_gains, 2 * bytes, "qk gains")) != PS_OK) return st;
     L.qk_norm = false;
@@ -370,7 +381,7 @@ extern "C" ps_status ps_verify_tokens(ps_ctx* c, const ps_tree* tree, const int3
     const char* name = "ps_verify_tokens";
     if (!c) return PS_EINVAL;
     ps_status st = check_tree(c, tree, name);
-    if (st != PS_OK) return st;
+    if (st != PS_OK || (st = check_not_captured(c, name)) != PS_OK) return st;
     ps_tree* t = const_cast<ps_tree*>(tree);   // its buffers for token ids
     const TreePlan& p = t->plan;
     const ps_model_desc& d = c->desc;

@@ -1,0 +1,63 @@
+"""Calls on drafted tokens around the kernels: what cannot be captured into a graph."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_17769_amd import binding as B
+from paper_2507_17769_amd.runner import Engine
+from test_gpu_tree import bf, load, make_batch, model_parts, random_tree
+
+pytestmark = pytest.mark.gpu
+
+
+def refused(status, call):
+    with pytest.raises(B.PolystepError) as e:
+        call()
+    assert e.value.status == status, str(e.value)
+
+
+def test_calls_with_work_on_the_host_are_refused_in_a_capture_and_leave_it_whole():
+    """ps_verify_tokens takes ids from the host, ps_tree_plan and ps_init_qk_norm keep what they are given on it: none of them is part of a graph.  What was
+    captured around them replays as ever, with steps over other ids in between, and those steps get what they get without a graph."""
+    rng = np.random.default_rng(23)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        V = 320
+        m, layers, head, gains = model_parts(2, V, 6)
+        spec = [(40, random_tree(rng, 9)), (7, [-1, 0, -2])]
+        seqs, parents, pages, n_pages = make_batch(rng, spec)
+        eng = Engine(m, n_pages, 2, 2, max_position=128)
+        load(eng, layers, head, gains)
+        eng.kv_pool().normal_()
+        tree, spare = eng.tree(seqs, parents), B.Tree(eng.ctx)
+        T = len(parents)
+        ids = [rng.integers(0, V, T).astype(np.int32) for _ in range(5)]
+        want = [{k: v.clone() for k, v in eng.verify_tokens(tree, i, want_logits=True).items()} for i in ids]
+        q = torch.randn(T, m["n_q"], m["head_dim"], device="cuda").to(torch.bfloat16)
+        z = torch.randn(T, V, device="cuda")
+        g = torch.ones(m["head_dim"], dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            o = eng.tree_attention(1, tree, q)
+            refused(B.PS_ESTATE, lambda: eng.ctx.verify_tokens(tree, ids[0]))
+            refused(B.PS_ESTATE, lambda: spare.plan(seqs, parents))
+            refused(B.PS_ESTATE, lambda: eng.ctx.init_qk_norm(1, g.data_ptr(), g.data_ptr()))
+            p = eng.pick_tokens(z)
+        for k in range(5):
+            got = eng.verify_tokens(tree, ids[k], want_logits=True)
+            o.fill_(3)
+            p["next"].fill_(-7)
+            graph.replay()
+            again = eng.verify_tokens(tree, ids[(k + 1) % 5], want_logits=True)
+            eager = eng.tree_attention(1, tree, q)
+            stream.synchronize()
+            assert all(torch.equal(got[n], want[k][n]) and torch.equal(again[n], want[(k + 1) % 5][n]) for n in got), k
+            assert torch.equal(p["next"], z.argmax(-1).to(torch.int32))
+            graph.replay()                         # the cache now holds what the last step appended
+            stream.synchronize()
+            assert torch.equal(o, eager), k
+        refused(B.PS_ESTATE, lambda: eng.tree_attention(0, spare, q[:0]))       # its plan was refused: it is empty
+        spare.plan(seqs, parents)
+        assert torch.equal(eng.tree_attention(1, spare, q), eager)
+        eng.close()
