@@ -321,6 +321,7 @@ ps_status ps_qk_norm_rope(ps_ctx* ctx, int32_t layer, const ps_tree* tree, const
  * keys and values are in the cache (ps_qk_norm_rope).  q, out: device bf16, T rows of n_q * head_dim values, ldq and ldo elements from
  * one row to the next, 16-byte aligned, rows too; they do not overlap.  Cache entries that a node does not see do not reach its row,
  * whatever they hold; a node's row depends on no other node's query.  Weights are rounded to bf16 for the matrix units, sums are fp32.
+ * A node whose scores are all -inf gets NaN.  Scores may lie anywhere within +-2^30 (fp32 sums have steps of 64 there).
  * Errors as ps_qk_norm_rope. */
 ps_status ps_tree_attention(ps_ctx* ctx, int32_t layer, const ps_tree* tree, const void* q, int64_t ldq, void* out, int64_t ldo);
 

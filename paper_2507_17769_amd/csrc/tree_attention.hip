@@ -214,7 +214,8 @@ __device__ __forceinline__ void matrix_results(f32x4_t& a, f32x4_t& b, f32x4_t& 
 constexpr u32x4_t ONES = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
 
 // End of an item: the NT tiles of a wavefront go to the output (normalised) or, for an item that covers only part of its KV span, to
-// partial slots it.partial + slot0 + nt.  l: each row's sum, the same in the four lanes that share the row.  Padding gets zeros.
+// partial slots it.partial + slot0 + nt.  l: each row's sum, the same in the four lanes that share the row.  Padding gets zeros, in a partial with
+// a weight of its own: a sum of zero is left to rows whose scores are all -inf, and their quotient, NaN, does not depend on how a plan cuts them.
 // Which 16 values of d accumulator dt holds: swapped accumulators (see team_pair) hold the neighbour's in the lanes of g >= 2.
 template <bool SWAP>
 __device__ __forceinline__ int dt_of(int dt, int g) { return SWAP ? dt ^ (g >> 1) : dt; }
@@ -248,7 +249,7 @@ __device__ __forceinline__ void store_rows(const TreeArgs& a, const AttnItem& it
             for (int dt = 0; dt < DT; dt++)
                 *reinterpret_cast<float4*>(po + 16 * dt_of<SWAP>(dt, g)) =
                     padding ? float4{0.f, 0.f, 0.f, 0.f} : float4{o[nt][dt][0], o[nt][dt][1], o[nt][dt][2], o[nt][dt][3]};
-            if (g == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * 16 + r) * 2) = padding ? float2{NEG_BIG, 0.f} : float2{m[nt], l[nt]};
+            if (g == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * 16 + r) * 2) = padding ? float2{NEG_BIG, 1.f} : float2{m[nt], l[nt]};
         }
     }
 }
@@ -661,7 +662,7 @@ __global__ __launch_bounds__(64 * TREE_WAVES) __attribute__((amdgpu_waves_per_eu
     }
 }
 
-// Combine split partials of one query tile: out = sum_j 2^(m_j - M) O_j / sum_j 2^(m_j - M) l_j, zeros where no split saw anything.
+// Combine split partials of one query tile: out = sum_j 2^(m_j - M) O_j / sum_j 2^(m_j - M) l_j.
 // One block per merge group, its wavefronts in a (pass, split) grid as in attn_merge_kernel.
 template <int D, int G>
 __global__ __launch_bounds__(64 * MERGE_MAX_WAVES) void tree_merge_kernel(TreeArgs a) {
@@ -726,7 +727,7 @@ __global__ __launch_bounds__(64 * MERGE_MAX_WAVES) void tree_merge_kernel(TreeAr
             }
         }
         if (ws == 0 && live) {
-            const float inv = L == 0.f ? 0.f : 1.0f / L;   // padding left zeros and sums of zero
+            const float inv = 1.0f / L;
             const int head = mg.kv_head * G + r % G, tok = mg.tok0 + r / G;
             uint2 w;
             w.x = pack_bf16(acc.x * inv, acc.y * inv);

@@ -1,5 +1,5 @@
 """Attention of token trees where the cache holds what a node sees and no finite sum can hide: infinities and NaN in the prefix, scores far from
-zero.  Oracle and tolerances are those of test_gpu_tree."""
+zero, rows whose scores are all -inf.  Oracle and tolerances are those of test_gpu_tree."""
 import numpy as np
 import pytest
 import torch
@@ -83,4 +83,37 @@ def test_equal_scores_far_from_zero_weigh_the_same(n_q, n_kv, d, sign, option):
             want, mag = V[see[i]].mean(0), np.abs(V[see[i]]).mean(0)
             assert (np.abs(got - want) <= HALF * np.abs(want) + (2 * see[i].sum() + 4) * EPS32 * mag * (1 + HALF)).all(), (p, i)
         t0 += len(t)
+    eng.close()
+
+
+@pytest.mark.parametrize("option", WIDE, ids=[str(o[1]) for o in WIDE])
+def test_rows_whose_scores_are_all_minus_infinity_are_nan(option):
+    """The softmax of nothing but -inf is not a number, however the plan cuts the row's keys; only padding, which sees nothing, is zero.  The other kv
+    head's rows are as ever."""
+    rng = np.random.default_rng(7)
+    spec = [(200, chain(1)), (0, [-1, -2]), (1500, random_tree(rng, 40, pad=3)), (640, [-1, 0]), (90, random_tree(rng, 9, pad=1))]
+
+    def edit(k, v, p, t):
+        k[:, 0] = 0.0
+        k[:, 0, 0] = float("-inf")
+    n_q, n_kv, d = 8, 2, 128
+
+    class Positive:
+        def standard_normal(self, shape):
+            x = rng.standard_normal(shape)
+            return np.abs(x) + 0.1 if len(shape) == 2 else x
+        permutation = staticmethod(rng.permutation)
+    eng, _, out, q, kv = run_attention(Positive(), n_q, n_kv, d, spec, [option], edit=edit)
+    pad = torch.from_numpy(np.concatenate([np.array(t) == B.PS_TREE_PAD for _, t in spec]))
+    assert torch.isnan(out[~pad][:, :4]).all() and not out[pad].any()
+    fine = [(k.clone(), v) for k, v in kv]
+    for k, _ in fine:
+        k[:, 0] = 0.0
+    t0 = 0
+    mended = out.clone()
+    for (p, t), (k, v) in zip(spec, fine):
+        n = len(t)
+        mended[t0:t0 + n, :4] = bf(ot.attention(f64(q[t0:t0 + n]), f64(k), f64(v), p, t)[0][:, :4])
+        t0 += n
+    check_attention(mended, q, fine, spec, d)
     eng.close()
