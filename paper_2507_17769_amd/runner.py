@@ -201,8 +201,8 @@ class Engine:
         """kept: for each sequence the nodes whose cache rows become the prefix's next positions, ascending."""
         self.ctx.tree_keep(tree, kept)
 
-    def _rules(self, rules, n_rows):
-        """rules: dict of device tensors with the names of ps_logit_rules ("mask" int32 [n_masks][words])."""
+    def _rules(self, rules, n_rows, vocab=0):
+        """rules: dict of device tensors with the names of ps_logit_rules ("mask" int32 [n_masks][words], whole words for `vocab` tokens)."""
         r, device, size = B.ps_logit_rules(), self.device, {}
         for name, t in rules.items():
             dtype = _RULE_TYPES.get(name)
@@ -236,7 +236,12 @@ class Engine:
                 raise ValueError(f"{name} must hold one entry per row")
         if r.mask:
             mask = rules["mask"]
-            r.n_masks, r.mask_stride = mask.shape[0], max(mask.shape[1], mask.stride(0))
+            r.n_masks, words = mask.shape
+            if words < (vocab + 31) // 32:
+                raise ValueError(f"mask holds {words} words a row, {vocab} tokens take {(vocab + 31) // 32}")
+            if r.n_masks > 1 and mask.stride(0) < words:
+                raise ValueError("the rows of mask overlap (mask_row gives several rows of logits one mask)")
+            r.mask_stride = mask.stride(0) if r.n_masks > 1 else words
         else:
             r.mask_row = None
         return r
@@ -251,7 +256,7 @@ class Engine:
         out = {"next": torch.empty(n, dtype=torch.int32, device=self.device), "logprob": torch.empty(n, dtype=torch.float32, device=self.device)}
         if want_logits:
             out["logits"] = torch.empty((n, vocab), dtype=torch.float32, device=self.device)
-        self.ctx.pick_tokens(p, _dtype_code(logits), ld, n, vocab, None if rules is None else self._rules(rules, n),
+        self.ctx.pick_tokens(p, _dtype_code(logits), ld, n, vocab, None if rules is None else self._rules(rules, n, vocab),
                              out["logits"].data_ptr() if want_logits else None, vocab, out["next"].data_ptr(), out["logprob"].data_ptr())
         return out
 
@@ -264,6 +269,6 @@ class Engine:
             out["logits"] = torch.empty((T, self.vocab), dtype=torch.float32, device=self.device)
         if want_hidden:
             out["hidden"] = torch.empty((T, self.model["hidden"]), dtype=torch.float32, device=self.device)
-        self.ctx.verify_tokens(tree, token_ids, None if rules is None else self._rules(rules, T), out["next"].data_ptr(), out["logprob"].data_ptr(),
+        self.ctx.verify_tokens(tree, token_ids, None if rules is None else self._rules(rules, T, getattr(self, "vocab", 0)), out["next"].data_ptr(), out["logprob"].data_ptr(),
                                out["logits"].data_ptr() if want_logits else None, out["hidden"].data_ptr() if want_hidden else None)
         return out

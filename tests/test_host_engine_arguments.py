@@ -1,0 +1,42 @@
+"""What Engine makes of the tensors of a call on drafted tokens, on the CPU: the pointers, counts and strides that the library gets, and what is refused
+because the library would read past a tensor.  No call reaches a device here."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_17769_amd import binding as B
+from paper_2507_17769_amd import workloads as W
+from paper_2507_17769_amd.runner import Engine
+
+
+def engine():
+    """An Engine as far as its checks of arguments go."""
+    e = Engine.__new__(Engine)
+    e.model, e.device = dict(W.MODELS["tiny"]), torch.device("cpu")
+    return e
+
+
+def words_read(r, n_rows, vocab, mask):
+    """The last word that picks of any row may read, counted from the start of the mask's storage."""
+    assert r.mask == mask.data_ptr()
+    return mask.storage_offset() + (r.n_masks - 1) * r.mask_stride + (vocab + 31) // 32
+
+
+@pytest.mark.parametrize("vocab", [1, 31, 32, 33, 1000])
+def test_masks_are_read_within_their_tensor(vocab):
+    e, words = engine(), (vocab + 31) // 32
+    wide = torch.zeros(7, words + 3, dtype=torch.int32)
+    for mask in (torch.zeros(5, words, dtype=torch.int32), wide, wide[:, :words], wide[1:6:2], wide[6:, 3:], wide[:1], torch.zeros(1, words, dtype=torch.int32)):
+        n = mask.shape[0]
+        r = e._rules({"mask": mask}, n, vocab)
+        assert r.n_masks == n and words_read(r, n, vocab, mask) <= mask.untyped_storage().nbytes() // 4
+        for i in range(n):
+            assert r.mask + 4 * i * r.mask_stride == mask[i].data_ptr() or n == 1
+    one = torch.zeros(1, words, dtype=torch.int32)
+    bad = [one.expand(6, words), torch.zeros(8 * words, dtype=torch.int32).as_strided((6, words), (0, 1))]
+    if words > 1:
+        bad += [torch.zeros(6 + words, dtype=torch.int32).as_strided((6, words), (1, 1)), torch.zeros(6, words - 1, dtype=torch.int32),
+                torch.zeros(6, words + 9, dtype=torch.int32)[:, :words - 1], torch.zeros(1, words - 1, dtype=torch.int32)]
+    for mask in bad:
+        with pytest.raises(ValueError):
+            e._rules({"mask": mask, "mask_row": torch.zeros(6, dtype=torch.int32)}, 6, vocab)
