@@ -234,16 +234,17 @@ class Engine:
         for name in _RULE_ROWS:
             if size.get(name, n_rows) != n_rows:
                 raise ValueError(f"{name} must hold one entry per row")
-        if r.mask:
-            mask = rules["mask"]
+        mask = rules.get("mask")
+        if mask is not None:
             r.n_masks, words = mask.shape
             if words < (vocab + 31) // 32:
                 raise ValueError(f"mask holds {words} words a row, {vocab} tokens take {(vocab + 31) // 32}")
             if r.n_masks > 1 and mask.stride(0) < words:
                 raise ValueError("the rows of mask overlap (mask_row gives several rows of logits one mask)")
+            if r.n_masks == 0 and not r.mask_row and n_rows:
+                raise ValueError("mask holds no rows, and no mask_row says which rows of logits have none")
+            r.mask = r.mask or r.mask_row      # of no rows: never read, but a mask_row of 0 or above has to find that it is not there
             r.mask_stride = mask.stride(0) if r.n_masks > 1 else words
-        else:
-            r.mask_row = None
         return r
 
     def pick_tokens(self, logits, rules=None, want_logits=False):

@@ -61,3 +61,16 @@ def test_calls_with_work_on_the_host_are_refused_in_a_capture_and_leave_it_whole
         spare.plan(seqs, parents)
         assert torch.equal(eng.tree_attention(1, spare, q), eager)
         eng.close()
+
+
+def test_rows_that_ask_for_a_mask_that_is_not_there():
+    eng = Engine("tiny", 1, max_position=16)
+    z = torch.randn(4, 5001, device="cuda")
+    rules = {"mask": torch.zeros(0, 157, dtype=torch.int32, device="cuda"), "mask_row": torch.tensor([-1, 0, 3, -5], dtype=torch.int32, device="cuda")}
+    got = eng.pick_tokens(z, rules, want_logits=True)
+    eng.ctx.sync()
+    top = z.argmax(-1).cpu().tolist()
+    assert got["next"].cpu().tolist() == [top[0], -1, -1, top[3]]
+    assert (got["logits"][1:3] == float("-inf")).all() and torch.equal(got["logits"][0], z[0]) and torch.equal(got["logits"][3], z[3])
+    refused(B.PS_EINVAL, lambda: eng.pick_tokens(z, {"mask_row": rules["mask_row"]}))
+    eng.close()

@@ -40,3 +40,18 @@ def test_masks_are_read_within_their_tensor(vocab):
     for mask in bad:
         with pytest.raises(ValueError):
             e._rules({"mask": mask, "mask_row": torch.zeros(6, dtype=torch.int32)}, 6, vocab)
+
+
+def test_a_mask_of_no_rows_allows_nothing_where_a_row_asks_for_one():
+    """mask_row at or above the number of masks: nothing is allowed, also where that number is 0; a mask_row without masks is the library's to refuse."""
+    e = engine()
+    none, row = torch.zeros(0, 4, dtype=torch.int32), torch.tensor([-1, 0, 2], dtype=torch.int32)
+    r = e._rules({"mask": none, "mask_row": row}, 3, 100)
+    assert r.mask and r.n_masks == 0 and r.mask_row == row.data_ptr() and r.mask_stride >= 4
+    with pytest.raises(ValueError):
+        e._rules({"mask": none}, 3, 100)
+    e._rules({"mask": none}, 0, 100)
+    r = e._rules({"mask_row": row}, 3, 100)
+    assert r.mask_row == row.data_ptr() and not r.mask
+    r = e._rules({"mask": None, "mask_row": None}, 3, 100)
+    assert not r.mask and not r.mask_row and r.n_masks == 0
