@@ -46,6 +46,9 @@ _RULE_ROWS = ("mask_row", "row_list", "row_token", "row_prev")
 
 
 class Engine:
+    """Work runs on the stream that is current when the engine is made.  A caller on another stream orders the two (wait_stream); the memory of tensors
+    that it hands over, and of results, is not handed out again before both streams are done with it."""
+
     def __init__(self, model, n_pool_pages, n_layers=1, n_kv_layers=1, max_position=None, perm_seed=0, device="cuda:0"):
         if not torch.cuda.is_available():
             raise RuntimeError("Engine needs a GPU: there is no CPU fallback")
@@ -54,6 +57,7 @@ class Engine:
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.stream = torch.cuda.current_stream(self.device)
+        self._stream_id = self.stream.cuda_stream, self.stream.device.index
         self.n_layers = n_layers
         if max_position is None:
             max_position = 16 * n_pool_pages
@@ -64,6 +68,25 @@ class Engine:
 
     def close(self):
         self.ctx.destroy()
+
+    def _elsewhere(self, *tensors):
+        """The current stream where it is not the engine's, else None; `tensors` are then marked as in use by the engine's."""
+        handle, index = self._stream_id
+        if torch._C._cuda_getCurrentRawStream(index) == handle:   # a number: a Stream object each time would cost a call as much as its checks
+            return None
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
+        return torch.cuda.current_stream(self.device)
+
+    def _empty(self, other, shape, dtype):
+        """A result's memory, the engine's stream's; `other`: what _elsewhere has said."""
+        if other is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(other)
+        return t
 
     def load_layer(self, layer, weights_bits):
         dev = {k: bits_to_dev(v, self.device) for k, v in weights_bits.items()}
@@ -80,12 +103,12 @@ class Engine:
     def step_tokens(self, seqs, token_ids, want_logits=True, want_hidden=False, want_stats=False, want_parts=False):
         """Full-model step.  Returns dict with "next" (int32 tensor [n_seqs]), optionally "logits" (fp32
         [n_seqs][vocab]) and "hidden" (fp32 [T][hidden]), "stats", "parts_ms"."""
-        n, T = len(seqs), sum(int(s.n_new) for s in seqs)
-        out = {"next": torch.empty(n, dtype=torch.int32, device=self.device)}
+        n, T, other = len(seqs), sum(int(s.n_new) for s in seqs), self._elsewhere()
+        out = {"next": self._empty(other, n, torch.int32)}
         if want_logits:
-            out["logits"] = torch.empty((n, self.vocab), dtype=torch.float32, device=self.device)
+            out["logits"] = self._empty(other, (n, self.vocab), torch.float32)
         if want_hidden:
-            out["hidden"] = torch.empty((T, self.model["hidden"]), dtype=torch.float32, device=self.device)
+            out["hidden"] = self._empty(other, (T, self.model["hidden"]), torch.float32)
         out["stats"], out["parts_ms"] = self.ctx.step_tokens(
             seqs, token_ids, out["next"].data_ptr(), out["logits"].data_ptr() if want_logits else None,
             out["hidden"].data_ptr() if want_hidden else None, want_stats, want_parts)
@@ -129,8 +152,9 @@ class Engine:
 
     def step(self, seqs, x_dev, out_dev=None, want_stats=False):
         """x_dev: int16 device tensor [T][hidden] of bf16 bits.  Returns (out_dev, stats)."""
+        other = self._elsewhere(x_dev, out_dev)
         if out_dev is None:
-            out_dev = torch.empty_like(x_dev)
+            out_dev = self._empty(other, x_dev.shape, x_dev.dtype)
         stats = self.ctx.step(seqs, x_dev.data_ptr(), out_dev.data_ptr(), want_stats)
         return out_dev, stats
 
@@ -179,8 +203,9 @@ class Engine:
         """qkv: [T][(n_q + 2 n_kv) * head_dim] fp32 or bf16, any row stride.  Appends keys and values; returns bf16 [T][n_q][head_dim]."""
         m = self.model
         p, ld = self._rows(qkv, tree.n_tokens, (m["n_q"] + 2 * m["n_kv"]) * m["head_dim"], "qkv")
+        other = self._elsewhere(qkv, q)
         if q is None:
-            q = torch.empty((tree.n_tokens, m["n_q"], m["head_dim"]), dtype=torch.bfloat16, device=self.device)
+            q = self._empty(other, (tree.n_tokens, m["n_q"], m["head_dim"]), torch.bfloat16)
         elif q.shape != (tree.n_tokens, m["n_q"], m["head_dim"]) or q.dtype != torch.bfloat16 or not q.is_contiguous() or q.device != self.device:
             raise ValueError("q must be a contiguous bf16 [T][n_q][head_dim] tensor of the engine's device")
         self.ctx.qk_norm_rope(layer, tree, p, _dtype_code(qkv), ld, q.data_ptr())
@@ -191,8 +216,9 @@ class Engine:
         m = self.model
         width = m["n_q"] * m["head_dim"]
         pq, ldq = self._rows(q, tree.n_tokens, width, "q", (torch.bfloat16,))
+        other = self._elsewhere(q, out)
         if out is None:
-            out = torch.empty((tree.n_tokens, m["n_q"], m["head_dim"]), dtype=torch.bfloat16, device=self.device)
+            out = self._empty(other, (tree.n_tokens, m["n_q"], m["head_dim"]), torch.bfloat16)
         po, ldo = self._rows(out, tree.n_tokens, width, "out", (torch.bfloat16,))
         self.ctx.tree_attention(layer, tree, pq, ldq, po, ldo)
         return out
@@ -254,9 +280,10 @@ class Engine:
             raise ValueError("logits must be [rows][vocab]")
         n, vocab = logits.shape
         p, ld = self._rows(logits, n, vocab, "logits")
-        out = {"next": torch.empty(n, dtype=torch.int32, device=self.device), "logprob": torch.empty(n, dtype=torch.float32, device=self.device)}
+        other = self._elsewhere(logits, *(rules or {}).values())
+        out = {"next": self._empty(other, n, torch.int32), "logprob": self._empty(other, n, torch.float32)}
         if want_logits:
-            out["logits"] = torch.empty((n, vocab), dtype=torch.float32, device=self.device)
+            out["logits"] = self._empty(other, (n, vocab), torch.float32)
         self.ctx.pick_tokens(p, _dtype_code(logits), ld, n, vocab, None if rules is None else self._rules(rules, n, vocab),
                              out["logits"].data_ptr() if want_logits else None, vocab, out["next"].data_ptr(), out["logprob"].data_ptr())
         return out
@@ -264,12 +291,12 @@ class Engine:
     def verify_tokens(self, tree, token_ids, rules=None, want_logits=False, want_hidden=False):
         """Full-model step over a batch of trees: token_ids host [T].  Returns {"next", "logprob"} for every node, optionally "logits"
         (changed by the rules) and "hidden"."""
-        T = tree.n_tokens
-        out = {"next": torch.empty(T, dtype=torch.int32, device=self.device), "logprob": torch.empty(T, dtype=torch.float32, device=self.device)}
+        T, other = tree.n_tokens, self._elsewhere(*(rules or {}).values())
+        out = {"next": self._empty(other, T, torch.int32), "logprob": self._empty(other, T, torch.float32)}
         if want_logits:
-            out["logits"] = torch.empty((T, self.vocab), dtype=torch.float32, device=self.device)
+            out["logits"] = self._empty(other, (T, self.vocab), torch.float32)
         if want_hidden:
-            out["hidden"] = torch.empty((T, self.model["hidden"]), dtype=torch.float32, device=self.device)
+            out["hidden"] = self._empty(other, (T, self.model["hidden"]), torch.float32)
         self.ctx.verify_tokens(tree, token_ids, None if rules is None else self._rules(rules, T, getattr(self, "vocab", 0)), out["next"].data_ptr(), out["logprob"].data_ptr(),
                                out["logits"].data_ptr() if want_logits else None, out["hidden"].data_ptr() if want_hidden else None)
         return out

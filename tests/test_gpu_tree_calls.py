@@ -1,9 +1,10 @@
-"""Calls on drafted tokens around the kernels: what cannot be captured into a graph."""
+"""Calls on drafted tokens around the kernels: what cannot be captured into a graph, tensors of another stream."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2507_17769_amd import binding as B
+from paper_2507_17769_amd import workloads as W
 from paper_2507_17769_amd.runner import Engine
 from test_gpu_tree import bf, load, make_batch, model_parts, random_tree
 
@@ -73,4 +74,70 @@ def test_rows_that_ask_for_a_mask_that_is_not_there():
     assert got["next"].cpu().tolist() == [top[0], -1, -1, top[3]]
     assert (got["logits"][1:3] == float("-inf")).all() and torch.equal(got["logits"][0], z[0]) and torch.equal(got["logits"][3], z[3])
     refused(B.PS_EINVAL, lambda: eng.pick_tokens(z, {"mask_row": rules["mask_row"]}))
+    eng.close()
+
+
+def busy(stream):
+    """More than half a second of work on a stream: what is enqueued behind it has not run when the call returns."""
+    with torch.cuda.stream(stream):
+        x = torch.ones(1 << 28, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(1300):
+            x.mul_(1.0)
+    return x
+
+
+def lies_free(address, size, dtype):
+    """The allocator hands memory at `address` out to the current stream."""
+    kept = [torch.empty(size, dtype=dtype, device="cuda") for _ in range(4)]
+    return address in [t.data_ptr() for t in kept]
+
+
+def test_tensors_dropped_after_a_call_from_another_stream_stay_until_it_has_run():
+    """An engine on one stream, calls made while another is current: the memory of temporaries and of results that are dropped at once is not handed out
+    before the engine's stream has come to its end."""
+    rng = np.random.default_rng(3)
+    stream = torch.cuda.Stream()
+    spec = [(60, random_tree(rng, 30)), (5, [-1])]
+    seqs, parents, pages, n_pages = make_batch(rng, spec)
+    seqs = [W.SeqSpec(*s) for s in seqs]
+    m, layers, head, gains = model_parts(1, 320, 2)
+    with torch.cuda.stream(stream):
+        eng = Engine(m, n_pages, 1, 1, max_position=256)
+        load(eng, layers, head, gains)
+        eng.kv_pool().normal_()
+    tree = eng.tree(seqs, parents)
+    T, n_q, n_kv, d, V = 31, m["n_q"], m["n_kv"], m["head_dim"], 70001
+    ids = rng.integers(0, 320, T).astype(np.int32)
+    eng.verify_tokens(tree, ids, want_logits=True)          # workspaces have their size: no call below waits for it
+    eng.step(seqs, torch.zeros(T, m["hidden"], dtype=torch.int16, device="cuda"))
+    eng.step_tokens(seqs, ids, want_hidden=True)
+    torch.cuda.synchronize()
+
+    def run(name, call, inputs):
+        torch.cuda.synchronize()
+        work = busy(stream)
+        held = [(t.data_ptr(), t.shape, t.dtype) for t in inputs]
+        out = call(*inputs)
+        results = list(out.values()) if isinstance(out, dict) else [out]
+        at = [(t.data_ptr(), t.shape, t.dtype) for t in results if torch.is_tensor(t)]
+        del out, results
+        inputs.clear()
+        again = [lies_free(*x) for x in held + at]
+        assert not stream.query(), f"{name}: the stream is idle, nothing was shown"
+        torch.cuda.synchronize()
+        del work
+        return again
+
+    odd = dict(device="cuda")
+    cases = {
+        "qk_norm_rope": (lambda qkv: eng.qk_norm_rope(0, tree, qkv), [torch.randn(T, (n_q + 2 * n_kv) * d, **odd)]),
+        "tree_attention": (lambda q: eng.tree_attention(0, tree, q), [torch.randn(T, n_q, d, **odd).to(torch.bfloat16)]),
+        "pick_tokens": (lambda z, p: eng.pick_tokens(z, {"presence": p}, want_logits=True), [torch.randn(T, V, **odd), torch.ones(T, **odd)]),
+        "verify_tokens": (lambda p: eng.verify_tokens(tree, ids, {"presence": p}, want_logits=True, want_hidden=True), [torch.ones(2, **odd)]),
+        "step": (lambda x: eng.step(seqs, x)[0], [torch.zeros(T, m["hidden"], dtype=torch.int16, **odd)]),
+        "step_tokens": (lambda: eng.step_tokens(seqs, ids, want_hidden=True), []),
+    }
+    for name, (call, inputs) in cases.items():
+        assert not any(run(name, call, inputs)), name
     eng.close()
