@@ -100,8 +100,8 @@ extern "C" ps_status ps_create(const ps_model_desc* desc, void* hip_stream, ps_c
     c->worker_slots = attention_worker_slots();
     st = dev_alloc(nullptr, &c->ws_pick, PICK_WORKSPACE_BYTES, "partial picks");
     if (st != PS_OK) { ps_destroy(c); return st; }
-    e = hipMemset(c->ws_pick, 0, PICK_WORKSPACE_BYTES);
-    if (e != hipSuccess) { ps_destroy(c); return hip_fail(nullptr, e, "hipMemset(partial picks)"); }
+    e = launch_fill_zero(c->ws_pick, PICK_WORKSPACE_BYTES, c->stream);   // ahead of every pick, which finds its counters at zero
+    if (e != hipSuccess) { ps_destroy(c); return hip_fail(nullptr, e, "partial picks"); }
     {   // set-up for ps_step_static, so that the entry point itself never allocates
         int dev = 0;
         e = hipGetDevice(&dev);
