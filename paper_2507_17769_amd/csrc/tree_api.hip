@@ -404,6 +404,7 @@ extern "C" ps_status ps_verify_tokens(ps_ctx* c, const ps_tree* tree, const int3
             return fail(c, PS_ERANGE, "ps_verify_tokens: token " + std::to_string(i) + " has id " + std::to_string(token_ids[i]) + " outside the vocabulary of " + std::to_string(V));
     return guarded(c, name, [&]() -> ps_status {
         OnDevice on(c);
+        c->step_counter++;
         if (!c->ws_embed && c->cap_tokens > 0) {  // workspaces were sized before the head existed
             HIP_TRY(c, hipStreamSynchronize(c->stream));
             free_workspaces(c);

@@ -1,4 +1,4 @@
-"""Calls on drafted tokens around the kernels: what cannot be captured into a graph, tensors of another stream."""
+"""Calls on drafted tokens around the kernels: what cannot be captured into a graph, tensors of another stream, options."""
 import numpy as np
 import pytest
 import torch
@@ -140,4 +140,19 @@ def test_tensors_dropped_after_a_call_from_another_stream_stay_until_it_has_run(
     }
     for name, (call, inputs) in cases.items():
         assert not any(run(name, call, inputs)), name
+    eng.close()
+
+
+def test_steps_over_trees_are_counted_like_others():
+    """Option time_attention = N: every Nth step, whatever kind it is."""
+    rng = np.random.default_rng(4)
+    m, layers, head, gains = model_parts(2, 320, 4)
+    seqs, parents, pages, n_pages = make_batch(rng, [(20, [-1, 0, 0])])
+    eng = Engine(m, n_pages, 2, 2, max_position=64)
+    load(eng, layers, head, gains)
+    tree = eng.tree(seqs, parents)
+    eng.ctx.set_option("time_attention", 3)
+    for _ in range(6):
+        eng.verify_tokens(tree, [1, 2, 3])
+    assert len(eng.ctx.attention_times()) == 2 * 2
     eng.close()
