@@ -313,7 +313,7 @@ ps_status ps_init_qk_norm(ps_ctx* ctx, int32_t layer, const void* g_q, const voi
 /* A layer's projections -> rotated queries, and keys and values in the cache: for each query and key head u' = u * gain / sqrt(mean(u^2) +
  * rms_eps) (layers with ps_init_qk_norm), rotated for the token's position; everything in fp32 and rounded to bf16 once.  qkv: device, T
  * rows of (n_q + 2 n_kv) * head_dim values of `dtype` (PS_F32 or PS_BF16), queries, keys, values, ld elements from one row to the next;
- * q: device bf16 [T][n_q][head_dim].  Both 16-byte aligned, rows of qkv too.
+ * q: device bf16 [T][n_q][head_dim].  Both 16-byte aligned, rows of qkv too; they do not overlap.
  * Errors: PS_EINVAL, PS_ERANGE (layer), PS_ESTATE (no plan, or one for another context or pool; no pool). */
 ps_status ps_qk_norm_rope(ps_ctx* ctx, int32_t layer, const ps_tree* tree, const void* qkv, int32_t dtype, int64_t ld, void* q);
 
@@ -362,7 +362,7 @@ typedef struct {
 /* Apply the rules to logits (device, n_rows rows of vocab <= 2^20 values of `dtype`, ld elements from one row to the next) and pick: next [n_rows]
  * the index of the largest, the lowest index among equal ones (a NaN is never it), or -1 where nothing is above -inf; logprob
  * [n_rows] fp32 its log-probability among the changed logits (-inf with next = -1; NaN if one of them is NaN or +inf); out fp32 the
- * changed logits, ldo elements from one row to the next (may be logits itself if that is fp32 and ld == ldo).  Outputs are device
+ * changed logits, ldo elements from one row to the next (may be logits itself if that is fp32 and ld == ldo, and overlaps them in no other way).  Outputs are device
  * memory, any may be null; rules null: none.  Needs no pool and no weights.  Errors: PS_EINVAL, PS_ERANGE, PS_ESTATE (host-only context). */
 ps_status ps_pick_tokens(ps_ctx* ctx, const void* logits, int32_t dtype, int64_t ld, int32_t n_rows, int32_t vocab, const ps_logit_rules* rules,
                          float* out, int64_t ldo, int32_t* next_tokens, float* logprobs);

@@ -62,6 +62,15 @@ ps_status guarded(ps_ctx* c, const char* name, F f) {
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// Whether n rows of two tensors share memory: bytes of a row, and from one to the next.  Rows of the same distance may lie between each other's.
+bool rows_meet(const void* a, int64_t row_a, int64_t step_a, const void* b, int64_t row_b, int64_t step_b, int64_t n) {
+    const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));   // of b behind a
+    if (d >= (n - 1) * step_a + row_a || -d >= (n - 1) * step_b + row_b) return false;
+    if (n == 1 || step_a != step_b) return true;
+    const int64_t at = (d % step_a + step_a) % step_a;
+    return at < row_a || at + row_b > step_a;
+}
+
 // A pinned buffer of at least `bytes` that nothing reads any more.
 ps_status pinned(ps_ctx* c, ps_tree::Pinned& b, size_t bytes) {
     if (b.pending) {
@@ -289,6 +298,8 @@ extern "C" ps_status ps_qk_norm_rope(ps_ctx* c, int32_t layer, const ps_tree* t,
     const size_t size = dtype == PS_F32 ? 4 : 2;
     if (ld < qkv_cols(c->desc)) return fail(c, PS_EINVAL, "ps_qk_norm_rope: ld is smaller than a row");
     if (!aligned(qkv, 16) || !aligned(q, 16) || (ld * size) % 16) return fail(c, PS_EINVAL, "ps_qk_norm_rope: qkv, its rows and q must be 16-byte aligned");
+    const int64_t q_row = (int64_t)c->desc.n_q_heads * c->desc.head_dim * 2;
+    if (rows_meet(qkv, qkv_cols(c->desc) * (int64_t)size, ld * (int64_t)size, q, q_row, q_row, t->plan.n_tokens)) return fail(c, PS_EINVAL, "ps_qk_norm_rope: qkv and q overlap");
     OnDevice on(c);
     const LayerWeights& L = c->layers[layer];
     const NormRopeArgs a{qkv, dtype == PS_BF16, 1, 0, ld, rope_out(c, t, layer, static_cast<bf16_t*>(q)), L.qk_norm ? L.qk_gains : nullptr, c->desc.rms_eps, t->plan.n_tokens};
@@ -306,6 +317,7 @@ extern "C" ps_status ps_tree_attention(ps_ctx* c, int32_t layer, const ps_tree* 
     const int row = c->desc.n_q_heads * c->desc.head_dim;
     if (ldq < row || ldo < row || ldq > INT32_MAX) return fail(c, PS_EINVAL, "ps_tree_attention: a row stride is smaller than a row, or ldq above 2^31 - 1");
     if (!aligned(q, 16) || !aligned(out, 16) || ldq % 8 || ldo % 8) return fail(c, PS_EINVAL, "ps_tree_attention: q, out and their rows must be 16-byte aligned");
+    if (rows_meet(q, row * 2, ldq * 2, out, row * 2, ldo * 2, t->plan.n_tokens)) return fail(c, PS_EINVAL, "ps_tree_attention: q and out overlap");
     OnDevice on(c);
     TreeArgs a = t->args;
     a.q = static_cast<const bf16_t*>(q); a.ldq = (int)ldq; a.pool_slot = slot_of(c, layer);
@@ -365,6 +377,10 @@ extern "C" ps_status ps_pick_tokens(ps_ctx* c, const void* logits, int32_t dtype
     if (ld < vocab || (out && ldo < vocab)) return fail(c, PS_EINVAL, "ps_pick_tokens: a row stride is smaller than a row");
     if (!aligned(logits, dtype == PS_F32 ? 4 : 2) || !aligned(out, 4) || !aligned(next_tokens, 4) || !aligned(logprobs, 4))
         return fail(c, PS_EINVAL, "ps_pick_tokens: a tensor is not aligned to its elements");
+    const int64_t size = dtype == PS_F32 ? 4 : 2;
+    const bool in_place = out == logits && dtype == PS_F32 && (ld == ldo || n_rows == 1);
+    if (out && !in_place && rows_meet(logits, vocab * size, ld * size, out, vocab * 4ll, ldo * 4, n_rows))
+        return fail(c, PS_EINVAL, "ps_pick_tokens: out overlaps logits and is not fp32 logits themselves");
     PickArgs a{logits, dtype == PS_BF16, ld, n_rows, vocab, ps_logit_rules{}, out, ldo, next_tokens, logprobs};
     if (rules) {
         const ps_status st = check_rules(c, *rules, n_rows, vocab, name);

@@ -1,4 +1,5 @@
-"""Calls on drafted tokens around the kernels: what cannot be captured into a graph, tensors of another stream, options."""
+"""Calls on drafted tokens around the kernels: what cannot be captured into a graph, tensors of another stream, options, results that
+overlap inputs."""
 import numpy as np
 import pytest
 import torch
@@ -155,4 +156,39 @@ def test_steps_over_trees_are_counted_like_others():
     for _ in range(6):
         eng.verify_tokens(tree, [1, 2, 3])
     assert len(eng.ctx.attention_times()) == 2 * 2
+    eng.close()
+
+
+def test_results_over_inputs_are_refused_where_they_would_be_read_again():
+    """Rows of one tensor may lie between another's; a result that shares memory with its input is refused, but for fp32 logits changed in place."""
+    m, layers, head, gains = model_parts(1, 320, 9)
+    eng = Engine(m, 4, 1, 1, max_position=64)
+    c, T, d = eng.ctx, 3, m["head_dim"]
+    wq, wqkv = m["n_q"] * d, (m["n_q"] + 2 * m["n_kv"]) * d
+    tree = eng.tree([(1, T, T, [2])], [-1, 0, 0])
+    buf = torch.randn(T, 2 * wqkv, device="cuda").to(torch.bfloat16)
+    P, row = buf.data_ptr(), 2 * wqkv
+    for out, ldo in ((P, row), (P + 2 * 8, row), (P + 2 * (wq - 8), row), (P + 2 * (row - wq + 8), row), (P + 2 * wq, row + 8), (P + 2 * (2 * row + wq - 8), row)):
+        refused(B.PS_EINVAL, lambda: c.tree_attention(0, tree, P, row, out, ldo))
+        refused(B.PS_EINVAL, lambda: c.tree_attention(0, tree, out, ldo, P, row))
+    q = buf[:, :wq].clone()
+    want = eng.tree_attention(0, tree, q)
+    for at in (wq, row - wq):                                       # between the rows of q
+        buf[:, :wq] = q
+        assert torch.equal(eng.tree_attention(0, tree, buf[:, :wq], buf[:, at:at + wq]), buf[:, at:at + wq]) and torch.equal(buf[:, at:at + wq].reshape(want.shape), want)
+    for q_at in (P, P + 2 * (2 * row + wqkv - 8), P - 2 * (T * wq - 8)):
+        refused(B.PS_EINVAL, lambda: c.qk_norm_rope(0, tree, P, B.PS_BF16, row, q_at))
+    V = 100
+    z = torch.randn(4, 2 * V, device="cuda")
+    Z = z.data_ptr()
+    for dtype, ld, n, out, ldo in ((B.PS_F32, 2 * V, 4, Z, V), (B.PS_F32, V, 4, Z, 2 * V), (B.PS_F32, 2 * V, 4, Z + 4, 2 * V), (B.PS_F32, 2 * V, 4, Z + 4 * (V - 1), 2 * V),
+                                   (B.PS_BF16, 2 * V, 4, Z, 2 * V), (B.PS_BF16, V, 1, Z, V), (B.PS_F32, V, 1, Z + 4, V), (B.PS_F32, 2 * V, 3, Z + 4 * (V + 1), 2 * V)):
+        refused(B.PS_EINVAL, lambda: c.pick_tokens(Z, dtype, ld, n, V, None, out, ldo))
+    logits, half = z[:, :V].clone(), z[:, :V].to(torch.bfloat16)
+    c.pick_tokens(Z, B.PS_F32, 2 * V, 4, V, None, Z + 4 * V, 2 * V)     # side by side
+    assert torch.equal(z[:, V:], logits)
+    c.pick_tokens(Z, B.PS_F32, 2 * V, 1, V, None, Z, 5 * V)             # one row, in place
+    z.view(torch.bfloat16)[:, :V] = half                              # bf16 rows of half the bytes, their results behind them
+    c.pick_tokens(Z, B.PS_BF16, 4 * V, 4, V, None, Z + 4 * V, 2 * V)
+    assert torch.equal(z[:, V:], half.float())
     eng.close()
