@@ -174,7 +174,7 @@ class Engine:
             raise ValueError(f"{name} must hold {n_rows} rows of {width}, not {tuple(shape)}")
         if n_rows and not adjacent:
             raise ValueError(f"the elements of a row of {name} must be adjacent")
-        return t.data_ptr(), (stride[0] if n_rows > 1 else max(width, stride[0]))
+        return t.data_ptr(), (stride[0] if n_rows > 1 else width)
 
     def kv_pool(self):
         """The KV pool as a bf16 tensor [KV slot][page][kv head][K, V][16 * head_dim] (a view: see ps_kv_pool for the order of a
@@ -200,7 +200,7 @@ class Engine:
         self.ctx.sync()
 
     def qk_norm_rope(self, layer, tree, qkv, q=None):
-        """qkv: [T][(n_q + 2 n_kv) * head_dim] fp32 or bf16, any row stride.  Appends keys and values; returns bf16 [T][n_q][head_dim]."""
+        """qkv: [T][(n_q + 2 n_kv) * head_dim] fp32 or bf16, rows anywhere on 16 bytes.  Appends keys and values; returns bf16 [T][n_q][head_dim]."""
         m = self.model
         p, ld = self._rows(qkv, tree.n_tokens, (m["n_q"] + 2 * m["n_kv"]) * m["head_dim"], "qkv")
         other = self._elsewhere(qkv, q)
@@ -212,7 +212,7 @@ class Engine:
         return q
 
     def tree_attention(self, layer, tree, q, out=None):
-        """q: bf16 [T][n_q][head_dim], any row stride; returns the same shape."""
+        """q: bf16 [T][n_q][head_dim], rows anywhere on 16 bytes; returns the same shape."""
         m = self.model
         width = m["n_q"] * m["head_dim"]
         pq, ldq = self._rows(q, tree.n_tokens, width, "q", (torch.bfloat16,))

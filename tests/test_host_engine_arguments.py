@@ -55,3 +55,12 @@ def test_a_mask_of_no_rows_allows_nothing_where_a_row_asks_for_one():
     assert r.mask_row == row.data_ptr() and not r.mask
     r = e._rules({"mask": None, "mask_row": None}, 3, 100)
     assert not r.mask and not r.mask_row and r.n_masks == 0
+
+
+def test_the_stride_of_a_single_row_does_not_matter():
+    e = engine()
+    wide = torch.zeros(3, 67, dtype=torch.bfloat16)
+    assert e._rows(wide[:, :64], 3, 64, "x") == (wide.data_ptr(), 67)
+    assert e._rows(wide[1:2, :64], 1, 64, "x") == (wide[1].data_ptr(), 64)      # 67 elements are no multiple of 16 bytes, and no row follows
+    assert e._rows(wide[:1, :64].view(1, 4, 16), 1, 64, "x") == (wide.data_ptr(), 64)
+    assert e._rows(torch.zeros(1, 64).expand(1, 64), 1, 64, "x")[1] == 64
