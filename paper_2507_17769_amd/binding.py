@@ -258,7 +258,8 @@ class Context:
             self.handle = None
 
     def __del__(self):
-        self.destroy()
+        if lib is not None:   # the interpreter ends, and this module has gone before its objects
+            self.destroy()
 
     def sync(self):
         self._check(lib.ps_sync(self.handle))
@@ -455,7 +456,8 @@ class Tree:
             self.handle = None
 
     def __del__(self):
-        self.destroy()
+        if lib is not None:   # the interpreter ends, and this module has gone before its objects
+            self.destroy()
 
 
 # ---- polysched: host-side consumers of the latency profile (include/polysched.h) -------------

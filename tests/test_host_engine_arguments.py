@@ -1,12 +1,17 @@
 """What Engine makes of the tensors of a call on drafted tokens, on the CPU: the pointers, counts and strides that the library gets, and what is refused
 because the library would read past a tensor.  No call reaches a device here."""
-import numpy as np
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
 from paper_2507_17769_amd import binding as B
 from paper_2507_17769_amd import workloads as W
 from paper_2507_17769_amd.runner import Engine
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def engine():
@@ -64,3 +69,18 @@ def test_the_stride_of_a_single_row_does_not_matter():
     assert e._rows(wide[1:2, :64], 1, 64, "x") == (wide[1].data_ptr(), 64)      # 67 elements are no multiple of 16 bytes, and no row follows
     assert e._rows(wide[:1, :64].view(1, 4, 16), 1, 64, "x") == (wide.data_ptr(), 64)
     assert e._rows(torch.zeros(1, 64).expand(1, 64), 1, 64, "x")[1] == 64
+
+
+def test_trees_that_outlive_the_binding_end_without_a_word():
+    """Objects in a cycle are collected when the interpreter ends, after the module whose functions free them."""
+    code = ("import sys\n"
+            "from paper_2507_17769_amd import binding as B\n"
+            "c = B.Context(256, 4, 2, 64, 256, host_only=True)\n"
+            "class Holder: pass\n"
+            "k = Holder()\n"
+            "k.tree, k.me = B.Tree(c).plan([(1, 1, 1, [0])]), k\n"
+            "sys.modules['holder'] = k\n"
+            "def g(x=k): return k\n"
+            "g.g, k.g = g, g\n")
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=120)
+    assert r.returncode == 0 and "Exception" not in r.stderr, r.stderr
