@@ -196,6 +196,9 @@ class Engine:
         gains = [g.to(device=self.device, dtype=torch.bfloat16).contiguous() for g in (g_q, g_k)]
         if any(g.shape != (d,) for g in gains):
             raise ValueError(f"gains must hold {d} elements")
+        other = self._elsewhere(*gains)
+        if other is not None:
+            self.stream.wait_stream(other)   # what the gains come from
         self.ctx.init_qk_norm(layer, gains[0].data_ptr(), gains[1].data_ptr())
         self.ctx.sync()
 

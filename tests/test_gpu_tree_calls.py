@@ -7,7 +7,7 @@ import torch
 from paper_2507_17769_amd import binding as B
 from paper_2507_17769_amd import workloads as W
 from paper_2507_17769_amd.runner import Engine
-from test_gpu_tree import bf, load, make_batch, model_parts, random_tree
+from test_gpu_tree import load, make_batch, make_engine, model_parts, random_tree
 
 pytestmark = pytest.mark.gpu
 
@@ -45,6 +45,7 @@ def test_calls_with_work_on_the_host_are_refused_in_a_capture_and_leave_it_whole
             refused(B.PS_ESTATE, lambda: eng.ctx.verify_tokens(tree, ids[0]))
             refused(B.PS_ESTATE, lambda: spare.plan(seqs, parents))
             refused(B.PS_ESTATE, lambda: eng.ctx.init_qk_norm(1, g.data_ptr(), g.data_ptr()))
+            refused(B.PS_ESTATE, lambda: eng.load_qk_norm(1, g, g))
             p = eng.pick_tokens(z)
         for k in range(5):
             got = eng.verify_tokens(tree, ids[k], want_logits=True)
@@ -191,4 +192,26 @@ def test_results_over_inputs_are_refused_where_they_would_be_read_again():
     z.view(torch.bfloat16)[:, :V] = half                              # bf16 rows of half the bytes, their results behind them
     c.pick_tokens(Z, B.PS_BF16, 4 * V, 4, V, None, Z + 4 * V, 2 * V)
     assert torch.equal(z[:, V:], half.float())
+    eng.close()
+
+
+def test_gains_are_taken_after_the_work_that_makes_them():
+    """load_qk_norm returns when the gains have been copied; they are copied behind the work of the caller's stream, which they come from."""
+    home, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(home):
+        eng = make_engine(4, 2, 64, 2)
+        tree = eng.tree([(1, 3, 3, [1])])
+        qkv = torch.randn(3, 8 * 64, device="cuda")
+        eng.load_qk_norm(0, torch.full((64,), 2.0, device="cuda"), torch.full((64,), 3.0, device="cuda"))
+        want = eng.qk_norm_rope(0, tree, qkv).clone()
+        gains = torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda")
+        eng.load_qk_norm(0, *gains)
+    torch.cuda.synchronize()
+    work = busy(other)
+    with torch.cuda.stream(other):
+        eng.load_qk_norm(0, gains[0].fill_(2.0), gains[1].fill_(3.0))
+    with torch.cuda.stream(home):
+        assert torch.equal(eng.qk_norm_rope(0, tree, qkv), want)
+    torch.cuda.synchronize()
+    del work
     eng.close()
