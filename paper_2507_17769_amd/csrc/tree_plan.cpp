@@ -7,7 +7,8 @@ namespace ps {
 static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // What a team takes for a pair of pages, in units of a third of what HBM takes to bring it to one of 256 compute units (0.7 us), by
-// the tiles of its query block.
+// the tiles of its query block.  Trees of one, six, 16 and 48 nodes side by side, us: 71, with 3 for all 72, with 3, 5 and 8 139 (70B
+// heads 87, 93 and 96); 24 trees of 16 beside two of 200: 80, 86 and 85.
 static int pair_weight(int tiles) { return tiles <= 4 ? 3 : tiles <= 8 ? 4 : 5; }
 
 // What a run takes besides its pairs, in pairs: to begin and to leave its rows (queries, page numbers and the first pages arrive, partials go),
@@ -52,7 +53,10 @@ static void build_tree_attention_plan(const PlanConfig& cfg, TreePlan& plan) {
     }
     if (pairs_team + pairs_wave == 0) return;
 
-    // Blocks: one to a compute unit, two where the runs are long enough (24 pairs a unit): twice the workers leave twice the partials.
+    // Blocks with teams: one to a compute unit, two where the runs are long enough (24 pairs a unit): twice the workers leave twice the partials.  One
+    // everywhere: 16 trees of 64 nodes 64 -> 75 us at 8B heads, 104 -> 125 at 70B; two everywhere: four trees of eight 18 -> 21 and 21 -> 27.
+    // Streaming wavefronts alone keep HBM busy from 13/16 of one block to a unit on, and leave fewer partials: single nodes behind 512 to 4096 tokens,
+    // 8, 32 and 128 sequences, 18.5, 46 and 190 us, with all units 19.8, 47 and 193; behind 100 to 700 tokens, 8 and 128 sequences, 13.7 and 45 for 13.7 and 46.
     const int cus = std::max(8, cfg.compute_units), places = std::max(2 * cus, cfg.block_slots);
     int64_t team_units = 0;
     for (int c = 1; c <= GANG; c++) team_units += units[c] * c;
@@ -61,7 +65,7 @@ static void build_tree_attention_plan(const PlanConfig& cfg, TreePlan& plan) {
         n_team = pairs_team ? cfg.n_workers : 0;
         n_wave = pairs_wave ? cfg.n_workers : 0;
     } else if (!pairs_team) {
-        n_wave = 4 * (pairs_wave >= 24 * (int64_t)pool[0].size() * cfg.n_kv_heads ? 13 * cus / 16 : cus);
+        n_wave = 4 * (13 * cus / 16);
     } else {
         const int blocks = pairs_team + pairs_wave / 4 < 24 * (int64_t)cus ? cus : places;
         n_team = blocks;
@@ -72,7 +76,7 @@ static void build_tree_attention_plan(const PlanConfig& cfg, TreePlan& plan) {
             n_wave = 4 * (blocks - n_team);
         }
     }
-    // in proportion to the work, in whole gangs, no run shorter than some four pairs
+    // in proportion to the work, in whole gangs, no run shorter than some four pairs (eight single nodes 18.4 us; two pairs the same, eight 19.6)
     for (int c = 1, left = n_team; c <= GANG; c++) {
         if (!units[c]) continue;
         int64_t pairs = 0;
