@@ -10,9 +10,9 @@
 // them, counts once, and moves each row's branch into the counts and out again, the next row's logits on their way.  The last block of a row
 // to finish joins the segments, in their order.  A block alone is a chain of trips to memory (its rows, what belongs to the list, the list and the
 // logits, the arrival), so it sends the loads of each trip together, and four blocks share a compute unit.
-// Measured (bf16 read, fp32 written, lists of 2000 tokens): 64 rows of 128256 in 30 us, 50 MB of which a copy takes 11; with empty lists 20.
-// fp32, 504 rows of 63-node trees in 76 us: 259 MB, 3.4 TB/s, where a plain read takes 43; a fifth goes to the segments of the frequent tokens.
-// One row: 8 us.  Counters of neighbouring rows in one line cost 8 us at 8 rows, loads under a lane's own condition twice the time at 64.
+// Measured, calls back to back (a kernel traced on its own takes 3 us more): 64 rows of 128256, bf16 read, fp32 written, lists of 2000 tokens, in 27 us,
+// 50 MB of which a copy takes 11; with empty lists 18.  fp32, 504 rows of 63-node trees in 72 us: 259 MB, 3.6 TB/s, where a plain read takes 43;
+// with empty lists 63.  One row: the kernel takes 8 us.  Counters of neighbouring rows in one line cost 8 us at 8 rows, loads under a lane's own condition twice the time at 64.
 
 #include "ps_device.h"
 

@@ -49,8 +49,9 @@ __device__ __forceinline__ uint32_t visible_word(const TreeArgs& a, const AttnIt
     const int left = it.pos0 + qc - 32 * pair;
     return left >= 31 ? 0xFFFFFFFFu : left < 0 ? 0u : (2u << left) - 1u;
 }
-// A team keeps the words of the first pairs that need them in LDS: a read from memory in the middle of the stream would wait for all the pages
-// on their way, 4 us a pair.
+// A team keeps the words of the first pairs that need them in LDS: a read from memory in the middle of the stream waits for all the pages
+// on their way.  Trees of up to some 100 nodes have no further pairs; eight trees of 512 behind 4000 tokens take 316 us where chains of
+// as many, whose words need no memory, take 302, one tree of 512 74 for 63.
 constexpr int MASK_PAIRS = 4, MASK_ROWS = 16 * TREE_WAVES * TREE_NT;   // words of a row, tokens of a block at most
 __device__ __forceinline__ uint32_t team_word(const TreeArgs& a, const AttnItem& it, const uint32_t* kept, int qc, int pair) {
     if (it.mask_at >= 0 && pair - it.mask_pair < MASK_PAIRS) return kept[(pair - it.mask_pair) * MASK_ROWS + qc];
@@ -172,8 +173,8 @@ __device__ __forceinline__ void hide(f32x4_t& sa, f32x4_t& sb, uint32_t word, in
 // have room for far more).  After an item's first pairs that hardly ever happens, and a pair then needs neither the maximum across the four
 // lanes of a row nor what came before rescaled, which took a third of the loop's vector instructions.  The row sums are taken from the
 // rounded P by the matrix unit, so that the weights of a row add up to one exactly as rounded.  What it costs: the largest weight is rounded like
-// the others, where below the maximum itself it is exactly 1 (measured: 0.0023 of the values off on average for 0.0020, 0.0017 of them the
-// rounding of the result).
+// the others, where against the maximum itself it is exactly 1.  Measured, against the maximum / as here: mean error of the values 1.9e-3 / 2.2e-3 of
+// them, 1.4e-3 of it the rounding of the result; 16 trees of 64 nodes, 64 heads, 176 / 157 us, 32 heads 105 / 97, 32 trees of 16 73 / 71.
 constexpr float OUTGROWN = 16.f;
 template <int DT>
 __device__ __forceinline__ bf16x8_t tile_softmax(const f32x4_t& sa, const f32x4_t& sb, float& m, f32x4_t (&o)[DT], f32x4_t& l, float scale2) {
