@@ -69,15 +69,19 @@ class Engine:
     def close(self):
         self.ctx.destroy()
 
-    def _elsewhere(self, *tensors):
-        """The current stream where it is not the engine's, else None; `tensors` are then marked as in use by the engine's."""
+    def _elsewhere(self):
+        """The current stream where it is not the engine's, else None."""
         handle, index = self._stream_id
         if torch._C._cuda_getCurrentRawStream(index) == handle:   # a number: a Stream object each time would cost a call as much as its checks
             return None
-        for t in tensors:
-            if t is not None:
-                t.record_stream(self.stream)
         return torch.cuda.current_stream(self.device)
+
+    def _lend(self, other, *tensors):
+        """Tensors of the caller's, checked, are about to be used by the engine's stream."""
+        if other is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
 
     def _empty(self, other, shape, dtype):
         """A result's memory, the engine's stream's; `other`: what _elsewhere has said."""
@@ -152,7 +156,8 @@ class Engine:
 
     def step(self, seqs, x_dev, out_dev=None, want_stats=False):
         """x_dev: int16 device tensor [T][hidden] of bf16 bits.  Returns (out_dev, stats)."""
-        other = self._elsewhere(x_dev, out_dev)
+        other = self._elsewhere()
+        self._lend(other, x_dev, out_dev)
         if out_dev is None:
             out_dev = self._empty(other, x_dev.shape, x_dev.dtype)
         stats = self.ctx.step(seqs, x_dev.data_ptr(), out_dev.data_ptr(), want_stats)
@@ -196,7 +201,7 @@ class Engine:
         gains = [g.to(device=self.device, dtype=torch.bfloat16).contiguous() for g in (g_q, g_k)]
         if any(g.shape != (d,) for g in gains):
             raise ValueError(f"gains must hold {d} elements")
-        other = self._elsewhere(*gains)
+        other = self._elsewhere()
         if other is not None:
             self.stream.wait_stream(other)   # what the gains come from
         self.ctx.init_qk_norm(layer, gains[0].data_ptr(), gains[1].data_ptr())
@@ -206,11 +211,12 @@ class Engine:
         """qkv: [T][(n_q + 2 n_kv) * head_dim] fp32 or bf16, rows anywhere on 16 bytes.  Appends keys and values; returns bf16 [T][n_q][head_dim]."""
         m = self.model
         p, ld = self._rows(qkv, tree.n_tokens, (m["n_q"] + 2 * m["n_kv"]) * m["head_dim"], "qkv")
-        other = self._elsewhere(qkv, q)
+        other = self._elsewhere()
         if q is None:
             q = self._empty(other, (tree.n_tokens, m["n_q"], m["head_dim"]), torch.bfloat16)
         elif q.shape != (tree.n_tokens, m["n_q"], m["head_dim"]) or q.dtype != torch.bfloat16 or not q.is_contiguous() or q.device != self.device:
             raise ValueError("q must be a contiguous bf16 [T][n_q][head_dim] tensor of the engine's device")
+        self._lend(other, qkv, q)
         self.ctx.qk_norm_rope(layer, tree, p, _dtype_code(qkv), ld, q.data_ptr())
         return q
 
@@ -219,10 +225,11 @@ class Engine:
         m = self.model
         width = m["n_q"] * m["head_dim"]
         pq, ldq = self._rows(q, tree.n_tokens, width, "q", (torch.bfloat16,))
-        other = self._elsewhere(q, out)
+        other = self._elsewhere()
         if out is None:
             out = self._empty(other, (tree.n_tokens, m["n_q"], m["head_dim"]), torch.bfloat16)
         po, ldo = self._rows(out, tree.n_tokens, width, "out", (torch.bfloat16,))
+        self._lend(other, q, out)
         self.ctx.tree_attention(layer, tree, pq, ldq, po, ldo)
         return out
 
@@ -283,23 +290,26 @@ class Engine:
             raise ValueError("logits must be [rows][vocab]")
         n, vocab = logits.shape
         p, ld = self._rows(logits, n, vocab, "logits")
-        other = self._elsewhere(logits, *(rules or {}).values())
+        r, other = None if rules is None else self._rules(rules, n, vocab), self._elsewhere()
+        self._lend(other, logits, *(rules or {}).values())
         out = {"next": self._empty(other, n, torch.int32), "logprob": self._empty(other, n, torch.float32)}
         if want_logits:
             out["logits"] = self._empty(other, (n, vocab), torch.float32)
-        self.ctx.pick_tokens(p, _dtype_code(logits), ld, n, vocab, None if rules is None else self._rules(rules, n, vocab),
+        self.ctx.pick_tokens(p, _dtype_code(logits), ld, n, vocab, r,
                              out["logits"].data_ptr() if want_logits else None, vocab, out["next"].data_ptr(), out["logprob"].data_ptr())
         return out
 
     def verify_tokens(self, tree, token_ids, rules=None, want_logits=False, want_hidden=False):
         """Full-model step over a batch of trees: token_ids host [T].  Returns {"next", "logprob"} for every node, optionally "logits"
         (changed by the rules) and "hidden"."""
-        T, other = tree.n_tokens, self._elsewhere(*(rules or {}).values())
+        T, other = tree.n_tokens, self._elsewhere()
+        r = None if rules is None else self._rules(rules, T, getattr(self, "vocab", 0))
+        self._lend(other, *(rules or {}).values())
         out = {"next": self._empty(other, T, torch.int32), "logprob": self._empty(other, T, torch.float32)}
         if want_logits:
             out["logits"] = self._empty(other, (T, self.vocab), torch.float32)
         if want_hidden:
             out["hidden"] = self._empty(other, (T, self.model["hidden"]), torch.float32)
-        self.ctx.verify_tokens(tree, token_ids, None if rules is None else self._rules(rules, T, getattr(self, "vocab", 0)), out["next"].data_ptr(), out["logprob"].data_ptr(),
+        self.ctx.verify_tokens(tree, token_ids, r, out["next"].data_ptr(), out["logprob"].data_ptr(),
                                out["logits"].data_ptr() if want_logits else None, out["hidden"].data_ptr() if want_hidden else None)
         return out

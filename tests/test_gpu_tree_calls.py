@@ -215,3 +215,19 @@ def test_gains_are_taken_after_the_work_that_makes_them():
     torch.cuda.synchronize()
     del work
     eng.close()
+
+
+def test_tensors_of_the_wrong_kind_are_refused_alike_from_every_stream():
+    eng = make_engine(4, 2, 64, 2)
+    tree = eng.tree([(1, 3, 3, [1])])
+    z, q = torch.zeros(3, 100, device="cuda"), torch.zeros(3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    for stream in (eng.stream, torch.cuda.Stream()):
+        with torch.cuda.stream(stream):
+            for error, call in ((ValueError, lambda: eng.qk_norm_rope(0, tree, torch.zeros(3, 512))), (ValueError, lambda: eng.qk_norm_rope(0, tree, torch.zeros(3, 512, device="cuda"), q.cpu())),
+                                (ValueError, lambda: eng.tree_attention(0, tree, q.cpu())), (ValueError, lambda: eng.tree_attention(0, tree, q, q.cpu())),
+                                (ValueError, lambda: eng.pick_tokens(z.cpu())), (TypeError, lambda: eng.pick_tokens(z, {"presence": torch.zeros(3)})),
+                                (TypeError, lambda: eng.pick_tokens(z, {"presence": torch.zeros(3, dtype=torch.int32, device="cuda")})),
+                                (ValueError, lambda: eng.pick_tokens(z, {"no_rule": z})), (TypeError, lambda: eng.verify_tokens(tree, [0, 0, 0], {"presence": torch.zeros(1)}))):
+                with pytest.raises(error):
+                    call()
+    eng.close()
